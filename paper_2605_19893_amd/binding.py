@@ -1,4 +1,4 @@
-"""Thin ctypes binding of libssv_nsa.so (include/ssv_nsa.h): argument marshalling only.
+"""Thin ctypes binding of libssv_nsa.so (include/ssv_nsa.h, include/ssv_round.h): argument marshalling only.
 
 Every step of the path runs in the HIP kernels behind the C ABI.  PyTorch appears here only as the
 owner of device memory and of the stream; nothing in this module computes on tensors.  There is
@@ -29,8 +29,11 @@ SSV_SCAN_AUTO, SSV_SCAN_STREAM, SSV_SCAN_MATRIX, SSV_SCAN_STREAM_TABLE = 0, 1, 2
 EXPORTS = ("ssv_nsa_verify", "ssv_nsa_verify_static", "ssv_nsa_verify_timed", "ssv_nsa_plan_query", "ssv_nsa_workspace_bytes",
            "ssv_nsa_supported", "ssv_nsa_strerror", "ssv_nsa_kernel_name", "ssv_nsa_version", "ssv_nsa_compress",
            "ssv_guard_default_config", "ssv_guard_init", "ssv_guard_observe", "ssv_tree_flatten")
+ROUND_EXPORTS = ("ssv_prefix_verify", "ssv_prefix_workspace_bytes", "ssv_sample", "ssv_sample_workspace_bytes", "ssv_accept",
+                 "ssv_commit")
 SSV_GUARD_MAX_CANDIDATES = 16
 SSV_TREE_BFS, SSV_TREE_DFS = 0, 1
+SSV_SAMPLE_MAX_V = 1 << 20
 
 
 class SsvNsaParams(ctypes.Structure):
@@ -47,6 +50,21 @@ class SsvCmpParams(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in
                 ("B", "H_kv", "d_k", "d_v", "l", "d", "dtype", "max_new_rows", "kv_capacity", "cmp_capacity")] + \
                [(n, ctypes.c_int64 * 3) for n in ("k_stride", "v_stride", "kc_stride", "vc_stride")]
+
+
+class SsvPrefixParams(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("B", "T", "H", "H_kv", "d_k", "d_v", "n_prefix", "dtype")] + \
+               [("scale", ctypes.c_float), ("max_prefix_len", ctypes.c_int32), ("max_seq_len", ctypes.c_int32)] + \
+               [(n, ctypes.c_int64 * 3) for n in ("kp_stride", "vp_stride", "k_stride", "v_stride", "q_stride", "out_stride")]
+
+
+class SsvSampleParams(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("B", "T", "V", "dtype")] + [("logits_stride", ctypes.c_int64 * 2)]
+
+
+class SsvCommitParams(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("layers", "B", "T", "H_kv", "d_k", "d_v", "dtype", "kv_capacity")] + \
+               [(n, ctypes.c_int64 * 4) for n in ("k_stride", "v_stride")]
 
 
 class SsvGuardConfig(ctypes.Structure):
@@ -121,6 +139,18 @@ def load_library() -> ctypes.CDLL:
                                          ctypes.POINTER(ctypes.c_int32), ctypes.POINTER(ctypes.c_int32)]
         lib.ssv_nsa_compress.restype = ctypes.c_int
         lib.ssv_nsa_compress.argtypes = [vp] * 4 + [i32p] * 3 + [ctypes.POINTER(SsvCmpParams), vp]
+        lib.ssv_prefix_verify.restype = ctypes.c_int
+        lib.ssv_prefix_verify.argtypes = [vp] * 5 + [i32p] * 4 + [ctypes.POINTER(SsvPrefixParams), vp, vp, ctypes.c_size_t, vp]
+        lib.ssv_prefix_workspace_bytes.restype = ctypes.c_size_t
+        lib.ssv_prefix_workspace_bytes.argtypes = [ctypes.POINTER(SsvPrefixParams)]
+        lib.ssv_sample.restype = ctypes.c_int
+        lib.ssv_sample.argtypes = [vp, vp, i32p, vp, vp, vp, i32p, ctypes.POINTER(SsvSampleParams), i32p, vp, vp, ctypes.c_size_t, vp]
+        lib.ssv_sample_workspace_bytes.restype = ctypes.c_size_t
+        lib.ssv_sample_workspace_bytes.argtypes = [ctypes.POINTER(SsvSampleParams)]
+        lib.ssv_accept.restype = ctypes.c_int
+        lib.ssv_accept.argtypes = [i32p] * 6 + [ctypes.c_int32] * 2 + [i32p] * 4 + [vp]
+        lib.ssv_commit.restype = ctypes.c_int
+        lib.ssv_commit.argtypes = [vp, vp] + [i32p] * 3 + [ctypes.POINTER(SsvCommitParams), vp]
         _lib = lib
     return _lib
 
@@ -255,3 +285,73 @@ def ssv_tree_flatten(parents, order: int):
     if rc != SSV_OK:
         raise SsvError(rc, "ssv_tree_flatten")
     return list(perm)[:n], list(newp)[:n]
+
+
+def make_prefix_params(*, B, T, H, H_kv, d_k, d_v, n_prefix=1, dtype=SSV_BF16, scale=0.0, max_prefix_len, max_seq_len,
+                       kp_stride=(0, 0, 0), vp_stride=(0, 0, 0), k_stride, v_stride, q_stride=(0, 0, 0),
+                       out_stride=(0, 0, 0)) -> SsvPrefixParams:
+    p = SsvPrefixParams(B=B, T=T, H=H, H_kv=H_kv, d_k=d_k, d_v=d_v, n_prefix=n_prefix, dtype=dtype, scale=scale,
+                        max_prefix_len=max_prefix_len, max_seq_len=max_seq_len)
+    for name, st in (("kp_stride", kp_stride), ("vp_stride", vp_stride), ("k_stride", k_stride), ("v_stride", v_stride),
+                     ("q_stride", q_stride), ("out_stride", out_stride)):
+        setattr(p, name, (ctypes.c_int64 * 3)(*[int(x) for x in st]))
+    return p
+
+
+def ssv_prefix_workspace_bytes(p: SsvPrefixParams) -> int:
+    return int(load_library().ssv_prefix_workspace_bytes(ctypes.byref(p)))
+
+
+def ssv_prefix_verify(q, k_prefix, v_prefix, k, v, prefix_lens, seq_lens, n_query, tree_parents, p: SsvPrefixParams, out,
+                      workspace, workspace_bytes: int, stream: int) -> None:
+    """Enqueue dense verification attention over shared prefixes and the sequences' own caches on `stream`."""
+    rc = load_library().ssv_prefix_verify(_ptr(q), _ptr(k_prefix), _ptr(v_prefix), _ptr(k), _ptr(v), _ptr(prefix_lens),
+                                          _ptr(seq_lens), _ptr(n_query), _ptr(tree_parents), ctypes.byref(p), _ptr(out),
+                                          _ptr(workspace), ctypes.c_size_t(int(workspace_bytes)), ctypes.c_void_p(int(stream)))
+    if rc != SSV_OK:
+        raise SsvError(rc, "ssv_prefix_verify")
+
+
+def make_sample_params(*, B, T, V, dtype, logits_stride=(0, 0)) -> SsvSampleParams:
+    p = SsvSampleParams(B=B, T=T, V=V, dtype=dtype)
+    p.logits_stride = (ctypes.c_int64 * 2)(*[int(x) for x in logits_stride])
+    return p
+
+
+def ssv_sample_workspace_bytes(p: SsvSampleParams) -> int:
+    return int(load_library().ssv_sample_workspace_bytes(ctypes.byref(p)))
+
+
+def ssv_sample(logits, temperature, top_k, top_p, min_p, u, n_query, p: SsvSampleParams, tokens, probs, workspace,
+               workspace_bytes: int, stream: int) -> None:
+    """Enqueue the sampling of one token per draft node from its logits and its given random number."""
+    rc = load_library().ssv_sample(_ptr(logits), _ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p), _ptr(u), _ptr(n_query),
+                                   ctypes.byref(p), _ptr(tokens), _ptr(probs), _ptr(workspace),
+                                   ctypes.c_size_t(int(workspace_bytes)), ctypes.c_void_p(int(stream)))
+    if rc != SSV_OK:
+        raise SsvError(rc, "ssv_sample")
+
+
+def ssv_accept(draft_tokens, root_tokens, sampled, seq_lens, n_query, tree_parents, B: int, T: int, path, n_accepted, next_tokens,
+               committed, stream: int) -> None:
+    """Enqueue the walk through the drafts that the sampled tokens accept."""
+    rc = load_library().ssv_accept(_ptr(draft_tokens), _ptr(root_tokens), _ptr(sampled), _ptr(seq_lens), _ptr(n_query),
+                                   _ptr(tree_parents), int(B), int(T), _ptr(path), _ptr(n_accepted), _ptr(next_tokens),
+                                   _ptr(committed), ctypes.c_void_p(int(stream)))
+    if rc != SSV_OK:
+        raise SsvError(rc, "ssv_accept")
+
+
+def make_commit_params(*, layers=1, B, T, H_kv, d_k, d_v, dtype, kv_capacity, k_stride, v_stride) -> SsvCommitParams:
+    p = SsvCommitParams(layers=layers, B=B, T=T, H_kv=H_kv, d_k=d_k, d_v=d_v, dtype=dtype, kv_capacity=kv_capacity)
+    p.k_stride = (ctypes.c_int64 * 4)(*[int(x) for x in k_stride])
+    p.v_stride = (ctypes.c_int64 * 4)(*[int(x) for x in v_stride])
+    return p
+
+
+def ssv_commit(k, v, path, n_accepted, seq_lens, p: SsvCommitParams, stream: int) -> None:
+    """Enqueue the move of the accepted draft rows of every layer to the front of the draft slots."""
+    rc = load_library().ssv_commit(_ptr(k), _ptr(v), _ptr(path), _ptr(n_accepted), _ptr(seq_lens), ctypes.byref(p),
+                                   ctypes.c_void_p(int(stream)))
+    if rc != SSV_OK:
+        raise SsvError(rc, "ssv_commit")

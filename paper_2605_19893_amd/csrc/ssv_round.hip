@@ -1,0 +1,285 @@
+// Host side of the C ABI declared in include/ssv_round.h: argument checks, launch planning and launches of the operators
+// around a verification round.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+
+#include "../../include/ssv_round.h"
+#include "k_accept.hpp"
+#include "k_prefix.hpp"
+#include "k_sample.hpp"
+
+namespace {
+
+using namespace ssv;
+
+int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
+size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
+bool misaligned(const void* p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to != 0; }
+
+// ---- shared-prefix attention
+constexpr int kPrefixMaxSlices = 32;       // per part (prefix, own rows)
+constexpr int kPrefixWgs = 512;            // one round of workgroups: two per CU
+
+struct PrefixPart {
+    int caches, per, rows, rb, n_rg, n_slices, n_wg;
+};
+
+struct PrefixLayout {
+    int H_g, es;
+    PrefixPart part[2];          // prefix (n_slices = 0: none), own rows
+    int n_slots;
+    int64_t rows_total;
+    int64_t q_s[3], out_s[3];    // bytes
+    size_t off_stats, off_acc, total;
+};
+
+// Slices that fill one round of workgroups, none shorter than two steps for each of a workgroup's wavefronts.
+int plan_part(PrefixPart* pt, int H_kv, int64_t max_keys) {
+    pt->rb = pt->rows > 32 ? 4 : (pt->rows > 16 ? 2 : 1);
+    pt->n_rg = ceil_div(pt->rows, 16 * pt->rb);
+    const int64_t groups = (int64_t)pt->caches * H_kv * pt->n_rg;
+    const int64_t by_keys = (max_keys + 8 * kPrefixStep - 1) / (8 * kPrefixStep);
+    pt->n_slices = (int)std::max<int64_t>(1, std::min<int64_t>({kPrefixWgs / groups, by_keys, kPrefixMaxSlices}));
+    if (groups * pt->n_slices > (1 << 24)) return SSV_EUNSUPPORTED;
+    pt->n_wg = (int)(groups * pt->n_slices);
+    return SSV_OK;
+}
+
+int prefix_layout(const ssv_prefix_params* p, PrefixLayout* lo) {
+    if (!p) return SSV_EINVAL;
+    if (p->B < 1 || p->T < 1 || p->H < 1 || p->H_kv < 1 || p->d_k < 1 || p->d_v < 1) return SSV_EINVAL;
+    if (p->H % p->H_kv || p->n_prefix < 1 || p->B % p->n_prefix) return SSV_EINVAL;
+    if (p->dtype != SSV_F32 && p->dtype != SSV_BF16) return SSV_EINVAL;
+    if (p->max_prefix_len < 0 || p->max_seq_len < 0 || !(p->scale >= 0.f) || std::isinf(p->scale)) return SSV_EINVAL;
+    const int H_g = p->H / p->H_kv;
+    if (p->T > SSV_MAX_T) return SSV_EUNSUPPORTED;
+    if (H_g != 1 && H_g != 2 && H_g != 4 && H_g != 8 && H_g != 16) return SSV_EUNSUPPORTED;
+    if (!ssv_nsa_supported(p->dtype, p->d_k, p->d_v)) return SSV_EUNSUPPORTED;
+    if (p->max_seq_len > INT32_MAX - SSV_MAX_T - 64 || p->max_prefix_len > INT32_MAX - 64) return SSV_EUNSUPPORTED;
+    const int es = p->dtype == SSV_BF16 ? 2 : 4;
+    const int64_t* strides[4] = {p->kp_stride, p->vp_stride, p->k_stride, p->v_stride};
+    for (int s = p->max_prefix_len ? 0 : 2; s < 4; ++s)
+        for (int j = 0; j < 3; ++j) {
+            if (strides[s][j] < 0 || strides[s][j] * es % 16) return SSV_EINVAL;
+            if (j == 2 && strides[s][j] < (s % 2 ? p->d_v : p->d_k)) return SSV_EINVAL;
+            // a step's rows are addressed by 32-bit offsets from its first one
+            if (j == 2 && strides[s][j] * es >= (1 << 26)) return SSV_EUNSUPPORTED;
+        }
+    std::memset(lo, 0, sizeof(*lo));
+    const int64_t* given[2] = {p->q_stride, p->out_stride};
+    int64_t* bytes[2] = {lo->q_s, lo->out_s};
+    const int dd[2] = {p->d_k, p->d_v};
+    for (int s = 0; s < 2; ++s) {
+        const bool dense = !given[s][0] && !given[s][1] && !given[s][2];
+        const int64_t st[3] = {dense ? (int64_t)p->T * p->H * dd[s] : given[s][0], dense ? (int64_t)p->H * dd[s] : given[s][1],
+                               dense ? dd[s] : given[s][2]};
+        for (int j = 0; j < 3; ++j) {
+            if (st[j] < 0 || st[j] * es % 16) return SSV_EINVAL;
+            bytes[s][j] = st[j] * es;
+        }
+        if (!dense && st[2] < dd[s] && p->H > 1) return SSV_EINVAL;
+    }
+    lo->H_g = H_g;
+    lo->es = es;
+    lo->rows_total = (int64_t)p->B * p->T * p->H;
+    if (lo->rows_total >= (1ll << 31)) return SSV_EUNSUPPORTED;
+    PrefixPart& shared = lo->part[0];
+    if (p->max_prefix_len) {
+        shared.caches = p->n_prefix;
+        shared.per = p->B / p->n_prefix;
+        shared.rows = shared.per * p->T * H_g;
+        if (const int rc = plan_part(&shared, p->H_kv, p->max_prefix_len)) return rc;
+    }
+    PrefixPart& own = lo->part[1];
+    own.caches = p->B;
+    own.per = 1;
+    own.rows = p->T * H_g;
+    if (const int rc = plan_part(&own, p->H_kv, (int64_t)p->max_seq_len + p->T)) return rc;
+    lo->n_slots = shared.n_slices + own.n_slices;
+    lo->off_stats = 0;
+    lo->off_acc = align_up((size_t)lo->n_slots * lo->rows_total * 8, 256);
+    lo->total = align_up(lo->off_acc + (size_t)lo->n_slots * lo->rows_total * p->d_v * 4, 256);
+    return SSV_OK;
+}
+
+template <bool BF16, int DK, int DV>
+int prefix_launch(const void* q, const void* kp, const void* vp, const void* k, const void* v, const int32_t* prefix_lens,
+                  const int32_t* seq_lens, const int32_t* n_query, const int32_t* parents, const ssv_prefix_params* p, void* out,
+                  char* ws, const PrefixLayout& lo, hipStream_t stream) {
+    const float scale = p->scale > 0.f ? p->scale : 1.f / std::sqrt((float)p->d_k);
+    for (int own = 0; own < 2; ++own) {
+        const PrefixPart& pt = lo.part[own];
+        if (!pt.n_slices) continue;
+        PrefixArgs a{};
+        a.q = (const char*)q;
+        a.k = (const char*)(own ? k : kp);
+        a.v = (const char*)(own ? v : vp);
+        a.lens = own ? seq_lens : prefix_lens;
+        a.n_query = n_query;
+        a.parents = parents;
+        a.part_stats = (float*)(ws + lo.off_stats);
+        a.part_acc = (float*)(ws + lo.off_acc);
+        a.T = p->T; a.H = p->H; a.H_kv = p->H_kv; a.H_g = lo.H_g;
+        a.per = pt.per; a.rows = pt.rows; a.n_rg = pt.n_rg;
+        a.own = own;
+        a.max_len = own ? p->max_seq_len : p->max_prefix_len;
+        a.n_slices = pt.n_slices;
+        a.slot0 = own ? lo.part[0].n_slices : 0;
+        a.min_steps = 2 * kPrefixWaves;
+        a.n_wg = pt.n_wg;
+        a.scale_log2 = scale * 1.4426950408889634f;
+        a.rows_total = lo.rows_total;
+        a.div_TH = FastDiv::of(p->T * lo.H_g);
+        a.div_Hg = FastDiv::of(lo.H_g);
+        for (int j = 0; j < 3; ++j) {
+            a.k_s[j] = (own ? p->k_stride : p->kp_stride)[j] * lo.es;
+            a.v_s[j] = (own ? p->v_stride : p->vp_stride)[j] * lo.es;
+            a.q_s[j] = lo.q_s[j];
+        }
+        const dim3 grid(align_up(pt.n_wg, 8));
+        switch (pt.rb) {
+            case 1: hipLaunchKernelGGL((k_prefix_stream<BF16, DK, DV, 1>), grid, dim3(kThreads), 0, stream, a); break;
+            case 2: hipLaunchKernelGGL((k_prefix_stream<BF16, DK, DV, 2>), grid, dim3(kThreads), 0, stream, a); break;
+            default: hipLaunchKernelGGL((k_prefix_stream<BF16, DK, DV, 4>), grid, dim3(kThreads), 0, stream, a); break;
+        }
+        if (hipGetLastError() != hipSuccess) return SSV_ELAUNCH;
+    }
+    PrefixCombineArgs c{};
+    c.part_stats = (const float*)(ws + lo.off_stats);
+    c.part_acc = (const float*)(ws + lo.off_acc);
+    c.n_query = n_query;
+    c.out = (char*)out;
+    c.T = p->T; c.H = p->H; c.n_slots = lo.n_slots;
+    c.rows_total = lo.rows_total;
+    c.div_H = FastDiv::of(p->H);
+    c.div_T = FastDiv::of(p->T);
+    for (int j = 0; j < 3; ++j) c.out_s[j] = lo.out_s[j];
+    hipLaunchKernelGGL((k_prefix_combine<BF16, DV>), dim3(ceil_div(lo.rows_total, kThreads / (DV / 4))), dim3(kThreads), 0, stream, c);
+    return hipGetLastError() == hipSuccess ? SSV_OK : SSV_ELAUNCH;
+}
+
+// ---- sampling
+int sample_check(const ssv_sample_params* p, int64_t s[2]) {
+    if (!p || p->B < 1 || p->T < 1 || p->V < 1) return SSV_EINVAL;
+    if (p->dtype != SSV_F32 && p->dtype != SSV_BF16) return SSV_EINVAL;
+    if (p->logits_stride[0] < 0 || p->logits_stride[1] < 0) return SSV_EINVAL;
+    if (p->V > SSV_SAMPLE_MAX_V || (int64_t)p->B * p->T >= (1ll << 31)) return SSV_EUNSUPPORTED;
+    const int es = p->dtype == SSV_BF16 ? 2 : 4;
+    const bool dense = !p->logits_stride[0] && !p->logits_stride[1];
+    s[0] = (dense ? (int64_t)p->T * p->V : p->logits_stride[0]) * es;
+    s[1] = (dense ? (int64_t)p->V : p->logits_stride[1]) * es;
+    return SSV_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t ssv_prefix_workspace_bytes(const ssv_prefix_params* p) {
+    PrefixLayout lo;
+    return prefix_layout(p, &lo) == SSV_OK ? lo.total : 0;
+}
+
+int ssv_prefix_verify(const void* q, const void* k_prefix, const void* v_prefix, const void* k, const void* v,
+                      const int32_t* prefix_lens, const int32_t* seq_lens, const int32_t* n_query, const int32_t* tree_parents,
+                      const ssv_prefix_params* p, void* out, void* workspace, size_t workspace_bytes, void* stream) {
+    PrefixLayout lo;
+    const int rc = prefix_layout(p, &lo);
+    if (rc != SSV_OK) return rc;
+    if (!q || !k || !v || !seq_lens || !out) return SSV_EINVAL;
+    if (p->max_prefix_len && (!k_prefix || !v_prefix || !prefix_lens)) return SSV_EINVAL;
+    const void* rows[] = {q, k, v, out, p->max_prefix_len ? k_prefix : nullptr, p->max_prefix_len ? v_prefix : nullptr};
+    for (const void* r : rows)
+        if (misaligned(r, 16)) return SSV_EINVAL;
+    const void* words[] = {p->max_prefix_len ? prefix_lens : nullptr, seq_lens, n_query, tree_parents};
+    for (const void* w : words)
+        if (misaligned(w, 4)) return SSV_EINVAL;
+    if (!workspace || misaligned(workspace, 256) || workspace_bytes < lo.total) return SSV_EWORKSPACE;
+#define SSV_DISPATCH(BF, DK, DV)                                                                                          \
+    if (p->dtype == ((BF) ? SSV_BF16 : SSV_F32) && p->d_k == (DK) && p->d_v == (DV))                                      \
+        return prefix_launch<BF, DK, DV>(q, k_prefix, v_prefix, k, v, prefix_lens, seq_lens, n_query, tree_parents, p, out, \
+                                         (char*)workspace, lo, (hipStream_t)stream);
+    SSV_DISPATCH(true, 192, 128)
+    SSV_DISPATCH(true, 128, 128)
+    SSV_DISPATCH(true, 64, 64)
+    SSV_DISPATCH(false, 64, 64)
+#undef SSV_DISPATCH
+    return SSV_EUNSUPPORTED;
+}
+
+size_t ssv_sample_workspace_bytes(const ssv_sample_params*) { return 0; }
+
+int ssv_sample(const void* logits, const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p,
+               const float* u, const int32_t* n_query, const ssv_sample_params* p, int32_t* tokens, float* probs, void*, size_t,
+               void* stream) {
+    SampleArgs a{};
+    const int rc = sample_check(p, a.s);
+    if (rc != SSV_OK) return rc;
+    if (!logits || !u || !tokens) return SSV_EINVAL;
+    if (misaligned(logits, p->dtype == SSV_BF16 ? 2 : 4)) return SSV_EINVAL;
+    const void* words[] = {temperature, top_k, top_p, min_p, u, n_query, tokens, probs};
+    for (const void* w : words)
+        if (misaligned(w, 4)) return SSV_EINVAL;
+    a.logits = (const char*)logits;
+    a.temperature = temperature; a.top_p = top_p; a.min_p = min_p; a.u = u; a.top_k = top_k; a.n_query = n_query;
+    a.tokens = tokens; a.probs = probs;
+    a.T = p->T; a.V = p->V;
+    int bits = 0;
+    while ((1 << bits) < p->V) ++bits;
+    a.mass_scale = std::ldexp(1.0, 62 - bits);
+    const dim3 grid(p->B * p->T);
+    if (p->dtype == SSV_BF16) hipLaunchKernelGGL(k_sample<true>, grid, dim3(kSampleThreads), 0, (hipStream_t)stream, a);
+    else hipLaunchKernelGGL(k_sample<false>, grid, dim3(kSampleThreads), 0, (hipStream_t)stream, a);
+    return hipGetLastError() == hipSuccess ? SSV_OK : SSV_ELAUNCH;
+}
+
+int ssv_accept(const int32_t* draft_tokens, const int32_t* root_tokens, const int32_t* sampled, const int32_t* seq_lens,
+               const int32_t* n_query, const int32_t* tree_parents, int32_t B, int32_t T, int32_t* path, int32_t* n_accepted,
+               int32_t* next_tokens, int32_t* committed, void* stream) {
+    if (B < 1 || T < 1) return SSV_EINVAL;
+    if (T > SSV_MAX_T) return SSV_EUNSUPPORTED;
+    if (!draft_tokens || !root_tokens || !sampled || !seq_lens || !path || !n_accepted || !next_tokens || !committed) return SSV_EINVAL;
+    const void* words[] = {draft_tokens, root_tokens, sampled, seq_lens, n_query, tree_parents, path, n_accepted, next_tokens, committed};
+    for (const void* w : words)
+        if (misaligned(w, 4)) return SSV_EINVAL;
+    const AcceptArgs a{draft_tokens, root_tokens, sampled, seq_lens, n_query, tree_parents, path, n_accepted, next_tokens, committed, B, T};
+    hipLaunchKernelGGL(k_accept, dim3(ceil_div(B, kThreads / 64)), dim3(kThreads), 0, (hipStream_t)stream, a);
+    return hipGetLastError() == hipSuccess ? SSV_OK : SSV_ELAUNCH;
+}
+
+int ssv_commit(void* k, void* v, const int32_t* path, const int32_t* n_accepted, const int32_t* seq_lens,
+               const ssv_commit_params* p, void* stream) {
+    if (!p || p->layers < 1 || p->B < 1 || p->T < 1 || p->H_kv < 1 || p->d_k < 1 || p->d_v < 1 || p->kv_capacity < 0) return SSV_EINVAL;
+    if (p->dtype != SSV_F32 && p->dtype != SSV_BF16) return SSV_EINVAL;
+    if (p->T > SSV_MAX_T) return SSV_EUNSUPPORTED;
+    const int es = p->dtype == SSV_BF16 ? 2 : 4;
+    if ((int64_t)p->d_k * es % 16 || (int64_t)p->d_v * es % 16) return SSV_EINVAL;
+    const int64_t* strides[2] = {p->k_stride, p->v_stride};
+    for (int s = 0; s < 2; ++s)
+        for (int j = 0; j < 4; ++j) {
+            if (strides[s][j] < 0 || strides[s][j] * es % 16) return SSV_EINVAL;
+            if (j == 3 && strides[s][j] < (s ? p->d_v : p->d_k)) return SSV_EINVAL;
+        }
+    if (!k || !v || !path || !n_accepted || !seq_lens || misaligned(k, 16) || misaligned(v, 16)) return SSV_EINVAL;
+    if (misaligned(path, 4) || misaligned(n_accepted, 4) || misaligned(seq_lens, 4)) return SSV_EINVAL;
+    CommitArgs a{};
+    a.k = (char*)k; a.v = (char*)v;
+    a.path = path; a.n_accepted = n_accepted; a.seq_lens = seq_lens;
+    a.B = p->B; a.T = p->T; a.H_kv = p->H_kv; a.cap = p->kv_capacity;
+    a.k_chunks = p->d_k * es / 16;
+    a.chunks = a.k_chunks + p->d_v * es / 16;
+    const int64_t pairs = (int64_t)p->layers * p->B * p->H_kv;
+    if (pairs >= (1ll << 31) || pairs * a.chunks >= (1ll << 38)) return SSV_EUNSUPPORTED;
+    a.total = pairs * a.chunks;
+    for (int j = 0; j < 4; ++j) {
+        a.k_s[j] = p->k_stride[j] * es;
+        a.v_s[j] = p->v_stride[j] * es;
+    }
+    hipLaunchKernelGGL(k_commit, dim3(ceil_div(a.total, kThreads)), dim3(kThreads), 0, (hipStream_t)stream, a);
+    return hipGetLastError() == hipSuccess ? SSV_OK : SSV_ELAUNCH;
+}
+
+}  // extern "C"

@@ -1,0 +1,188 @@
+"""Sampling against its definition in 64 bits: the token is the definition's, except where the given number lies within the
+rounding of a border (2^-40 of the kept sum, which 2^20 roundings of 2^-53 and the filters' fixed-point sums stay far below);
+the probability is off by its one rounding to fp32 and 2^-40."""
+import numpy as np
+import pytest
+
+import round_oracle as ro
+
+pytestmark = pytest.mark.gpu
+
+
+def run(x, t=None, k=None, p=None, m=None, u=None, nq=None, stride=(0, 0), probs=True):
+    """x: device tensor [B, T, V] (or a view); per-sequence lists; u [B, T]."""
+    import torch
+    from paper_2605_19893_amd import binding as Bd
+    B, T, V = x.shape
+    dev = lambda v, dt: None if v is None else torch.tensor(v, dtype=dt, device="cuda")
+    prm = Bd.make_sample_params(B=B, T=T, V=V, dtype=Bd.SSV_BF16 if x.dtype == torch.bfloat16 else Bd.SSV_F32,
+                                logits_stride=stride)
+    need = Bd.ssv_sample_workspace_bytes(prm)
+    ws = torch.full((max(need, 1),), 0x55, dtype=torch.uint8, device="cuda")
+    tokens = torch.full((B, T), -9, dtype=torch.int32, device="cuda")
+    pr = torch.full((B, T), -9.0, device="cuda") if probs else None
+    Bd.ssv_sample(x, dev(t, torch.float32), dev(k, torch.int32), dev(p, torch.float32), dev(m, torch.float32),
+                  torch.as_tensor(np.asarray(u, np.float32)).cuda(), dev(nq, torch.int32), prm, tokens, pr, ws if need else None, need,
+                  torch.cuda.current_stream().cuda_stream)
+    torch.cuda.synchronize()
+    return tokens.cpu().numpy(), None if pr is None else pr.double().cpu().numpy()
+
+
+def check(x, t, k, p, m, u, nq=None, **kw):
+    """x: device tensor; every row against the definition."""
+    tok, pr = run(x, t, k, p, m, u, nq, **kw)
+    h = x.double().cpu().numpy()
+    f32 = lambda v, d: np.float64(np.float32(d if v is None else v))
+    for b in range(h.shape[0]):
+        for i in range(h.shape[1]):
+            if nq is not None and i >= nq[b]:
+                assert tok[b, i] == -1 and pr[b, i] == 0
+                continue
+            want, prob, margin = ro.sample(h[b, i], f32(None if t is None else t[b], 1), 0 if k is None else k[b], f32(None if p is None else p[b], 1),
+                                           f32(None if m is None else m[b], 0), float(np.float32(u[b][i])))
+            if margin > 2.0 ** -40:
+                assert tok[b, i] == want, (b, i, tok[b, i], want, margin)
+                assert abs(pr[b, i] - prob) <= (2.0 ** -24 + 2.0 ** -40) * prob, (b, i, pr[b, i], prob)
+
+
+def logits(seed, shape, dtype, tail=0.5):
+    import torch
+    g = torch.Generator().manual_seed(seed)
+    z = torch.randn(shape, generator=g)
+    return (2.0 * z + tail * z.clamp_min(0) ** 2).to(torch.bfloat16 if dtype == "bf16" else torch.float32).cuda()
+
+
+SETTINGS = [(1.0, 0, 1.0, 0.0), (0.8, 0, 0.95, 0.0), (0.7, 40, 0.9, 0.02), (0.0, 0, 1.0, 0.0), (1.5, 1000, 0.99, 0.001), (2.0, 5, 1.0, 0.0),
+            (1.0, 0, 1.0, 0.1), (0.3, 0, 0.5, 0.0), (1.0, 1, 1.0, 0.0), (5.0, 0, 0.999, 0.0), (1.0, 3000, 0.9999, 0.0), (0.01, 0, 0.9, 0.3)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("V", [1, 2, 7, 64, 1000, 8191, 8192, 8193, 32000, 50001, 131071])
+def test_settings_over_vocabularies(dtype, V):
+    rng = np.random.default_rng(V)
+    B = len(SETTINGS)
+    x = logits(V, (B, 2, V), dtype)
+    t, k, p, m = (list(c) for c in zip(*SETTINGS))
+    check(x, t, k, p, m, rng.random((B, 2)))
+
+
+def test_neutral_settings_by_null_pointers_and_no_probabilities():
+    rng = np.random.default_rng(5)
+    x = logits(5, (3, 4, 777), "f32")
+    u = rng.random((3, 4))
+    check(x, None, None, None, None, u)
+    a, _ = run(x, u=u)
+    b, none = run(x, u=u, probs=False)
+    assert none is None and np.array_equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_ties_go_to_the_lowest_index(dtype):
+    """Values from a handful: the threshold falls inside a class of equal logits, whose first indices are kept."""
+    import torch
+    g = torch.Generator().manual_seed(3)
+    x = torch.randint(0, 5, (8, 2, 20011), generator=g).float().to(torch.bfloat16 if dtype == "bf16" else torch.float32).cuda()
+    rng = np.random.default_rng(3)
+    check(x, [1.0] * 8, [1, 7, 100, 4001, 9000, 0, 0, 4500], [1.0, 1.0, 1.0, 1.0, 0.7, 0.3, 0.9, 0.77], [0, 0, 0, 0, 0, 0, 0.2, 0.3], rng.random((8, 2)))
+
+
+def test_all_equal_logits():
+    import torch
+    x = torch.full((5, 1, 640), -2.5, dtype=torch.bfloat16, device="cuda")
+    u = [[0.05], [0.55], [0.95], [0.999], [0.0]]
+    tok, pr = run(x, [1.0] * 5, [10] * 5, None, None, u)
+    assert tok[:, 0].tolist() == [0, 5, 9, 9, 0] and np.allclose(pr, 0.1, rtol=1e-6)
+    tok, _ = run(x, [1.0] * 5, None, None, None, u)
+    assert tok[:, 0].tolist() == [32, 352, 607, 639, 0]      # (0.95 in fp32 is 0.94999999: 607.99999 of 640)
+
+
+def test_masked_infinite_and_nan_logits():
+    import torch
+    inf, nan = float("inf"), float("nan")
+    rows = [[-inf] * 9, [nan] * 9, [-inf, 1.0, -inf, 1.0, -inf, nan, 1.0, -inf, -inf], [0.0, inf, 3.0, inf, -inf, nan, 1.0, 2.0, 5.0],
+            [-3.4028235e38, -inf, -3.4028235e38, -inf, -inf, -inf, -inf, -inf, nan], [-0.0, 0.0, -0.0, 0.0, -1.0, -1.0, -inf, -inf, -inf]]
+    for dt in (torch.float32, torch.bfloat16):
+        x = torch.tensor(rows, dtype=dt).reshape(6, 1, 9).repeat(1, 4, 1).cuda()
+        u = [[0.0, 0.3, 0.7, 0.999]] * 6
+        for t, k, p, m in [(1.0, 0, 1.0, 0.0), (0.0, 0, 1.0, 0.0), (0.5, 2, 1.0, 0.0), (0.5, 0, 0.6, 0.0), (2.0, 0, 1.0, 0.5), (1.0, 8, 0.9, 0.9), (1.0, 3, 0.7, 1.0)]:
+            check(x, [t] * 6, [k] * 6, [p] * 6, [m] * 6, u)
+        tok, pr = run(x, [1.0] * 6, None, None, None, u)
+        assert (tok[:2] == -1).all() and (pr[:2] == 0).all()
+        assert set(tok[2]) <= {1, 3, 6} and set(tok[3]) <= {1, 3}
+        # the lowest finite fp32 value lies beyond the largest of bf16, (2 - 2^-7) 2^127, and rounds to -inf there
+        assert set(tok[4]) <= ({0, 2} if dt == torch.float32 else {-1})
+
+
+def test_odd_settings():
+    """What the documentation says of values out of range."""
+    nan = float("nan")
+    x = logits(9, (12, 1, 3001), "f32")
+    t = [-1.0, nan, 1.0, 1.0, 1.0, 1.0, 1.0, 1.0, 1e-30, 1e30, float("inf"), 1e-45]
+    k = [0, 0, -4, 99999, 0, 0, 0, 0, 0, 0, 0, 0]
+    p = [1.0, 1.0, 1.0, 1.0, nan, -0.5, 0.0, 7.0, 0.9, 0.9, 1.0, 1.0]
+    m = [0.0, 0.0, 0.0, 0.0, nan, 0.0, 0.0, 3.0, 0.0, 0.0, 0.0, 0.0]
+    check(x, t, k, p, m, np.random.default_rng(9).random((12, 1)))
+
+
+def test_random_numbers_at_the_ends():
+    x = logits(10, (5, 1, 5000), "bf16")
+    x[:, :, 4000:] = float("-inf")
+    u = [[0.0], [1.0], [float("nan")], [-3.0], [np.nextafter(np.float32(1), np.float32(0))]]
+    check(x, [1.0] * 5, [0] * 5, [1.0, 1.0, 0.9, 0.9, 0.9], [0.0] * 5, u)
+
+
+def test_strides_ragged_counts_and_unaligned_rows():
+    """Rows that start at every alignment, a padded vocabulary, nodes that do not exist (their logits are not read)."""
+    import torch
+    B, T, V = 4, 5, 1501
+    for dt in ("bf16", "f32"):
+        h = logits(21, (B, T, V), dt)
+        for off in range(0, 8):
+            buf = torch.full((B * T * (V + 13) + 64,), 50.0, dtype=h.dtype, device="cuda")
+            x = buf[off:].as_strided((B, T, V), (T * (V + 13), V + 13, 1), off)
+            x.copy_(h)
+            x[1, 3:] = 1000.0
+            check(x, [0.9] * B, [0, 20, 0, 0], [0.9, 1.0, 1.0, 0.5], [0.0, 0.0, 0.01, 0.0], np.random.default_rng(off).random((B, T)),
+                  nq=[5, 3, 0, 1], stride=x.stride()[:2])
+
+
+def test_graph_replays_and_another_stream():
+    import torch
+    from paper_2605_19893_amd import binding as Bd
+    x = logits(31, (4, 3, 9001), "bf16")
+    u = torch.rand((4, 3), device="cuda")
+    t, p = torch.full((4,), 0.9, device="cuda"), torch.full((4,), 0.9, device="cuda")
+    prm = Bd.make_sample_params(B=4, T=3, V=9001, dtype=Bd.SSV_BF16)
+    need = Bd.ssv_sample_workspace_bytes(prm)
+    ws = torch.full((max(need, 1),), 0x55, dtype=torch.uint8, device="cuda")
+    tok, pr = torch.empty((4, 3), dtype=torch.int32, device="cuda"), torch.empty((4, 3), device="cuda")
+    go = lambda s: Bd.ssv_sample(x, t, None, p, None, u, None, prm, tok, pr, ws, need, s.cuda_stream)
+    go(torch.cuda.current_stream())
+    want = tok.clone(), pr.clone()
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        go(s)
+    for _ in range(3):
+        tok.fill_(-7)
+        ws.fill_(0x55)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(tok, want[0]) and torch.equal(pr, want[1])
+        torch.randn(1000, device="cuda").sum().item()
+
+
+def test_frequencies_follow_the_probabilities():
+    """Evenly spaced numbers give every kept token its share, to within one number."""
+    n = 4096
+    x = logits(41, (1, 1, 50), "f32").expand(1, n, 50)
+    u = ((np.arange(n) + 0.5) / n)[None]
+    tok, _ = run(x, [1.0], [0], [0.95], [0.0], u, stride=(50, 0))
+    h = x[0, 0].double().cpu().numpy()
+    order = np.argsort(-h, kind="stable")
+    w = np.exp(h - h.max())
+    keep = np.cumsum(w[order]) - w[order] < float(np.float32(0.95)) * w.sum()
+    share = np.zeros(50)
+    share[order[keep]] = w[order[keep]] / w[order[keep]].sum()
+    assert (np.abs(np.bincount(tok[0], minlength=50) - n * share) <= 1.0 + 1e-6).all()
