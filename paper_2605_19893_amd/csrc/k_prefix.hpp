@@ -5,34 +5,52 @@
 // is split over slices of keys; every slice leaves a partial softmax state (m, Z = sum 2^(x - m), sum 2^(x - m) v) per row and
 // k_prefix_combine joins them.  The rows that meet a prefix are those of all its sequences, stacked: row r of a (prefix, KV
 // head) pair is (sequence, node, head of the group) = (r / (T H_g), r / H_g % T, r % H_g), so a prefix row is read once for
-// up to 16 RB rows of the batch.  The rows that meet a sequence's own keys are the same with one sequence.
+// all rows of a workgroup.  The rows that meet a sequence's own keys are the same with one sequence.
+//
+// One launch holds the workgroups of both parts, each on the path that its row count asks for:
+//   rows path (prefix_rows, bf16, more than 16 rows): up to 256 rows share every key tile through LDS, one block of 32 rows per
+//     wavefront on the 32x32x16 matrix instruction: bound by the matrix cores when the rows are many;
+//   keys path (prefix_keys): 16 rows (fp32: up to 32); the wavefronts divide the keys instead, nothing is shared: bound by memory.
 #pragma once
+#include <type_traits>
+
 #include "device_common.hpp"
 
 namespace ssv {
 
+struct PrefixPart {
+    const char *k, *v;                 // the prefixes, or the sequences' own caches
+    const int32_t* lens;               // rows of each prefix, or committed tokens of each sequence
+    int per;                           // sequences that share a cache (1: the sequences' own)
+    int rows, n_rg;                    // rows per (cache, KV head); groups of them, one per workgroup
+    int max_len;
+    int n_slices, slot0;               // slices per pair, and the first one's partial-state slot
+    int n_wg, n_pad;                   // workgroups, and the same rounded up to a multiple of 8
+    int64_t k_s[3], v_s[3];            // bytes: cache, KV head, row
+};
+
 struct PrefixArgs {
-    const char *q, *k, *v;             // k, v: the prefixes or the sequences' own caches
-    const int32_t *lens;               // rows of each prefix, or committed tokens of each sequence
+    PrefixPart part[2];                // prefix, own
+    const char* q;
     const int32_t *n_query, *parents;
     float *part_stats, *part_acc;
     int T, H, H_kv, H_g;
-    int per;                           // sequences that share a cache (1: the sequences' own)
-    int rows, n_rg;                    // rows per (cache, KV head); groups of 16 RB of them
-    int own;                           // 1: own caches: draft rows behind the committed ones, visible by ancestry
-    int max_len;
-    int n_slices, slot0;               // slices per pair, and the first one's partial-state slot
-    int min_steps;                     // key steps a slice holds at least
-    int n_wg;                          // workgroups (the grid is padded to a multiple of 8)
     float scale_log2;
     int64_t rows_total;
     FastDiv div_TH, div_Hg;
-    int64_t k_s[3], v_s[3];            // bytes: cache, KV head, row
     int64_t q_s[3];                    // bytes: sequence, node, head
 };
 
-constexpr int kPrefixStep = 32;        // keys per step of a wavefront
-constexpr int kPrefixWaves = kThreads / 64;
+constexpr int kPrefixThreads = 512;
+constexpr int kPrefixWaves = kPrefixThreads / 64;
+constexpr int kPrefixStep = 32;        // keys per step of a wavefront on the keys path
+constexpr int kPrefixMinTiles = 2;     // tiles of 64 keys that a slice holds at least
+constexpr float kPrefixRaiseLog2 = 8.f;   // the reference maximum follows the running one at a distance of up to 2^8
+
+struct PrefixTree {                    // LDS: the draft tree of one sequence
+    AncSet anc[kMaxT];
+    int par[kMaxT];
+};
 
 // Ancestors-or-self of every node of one sequence (the set bits of s_anc[i]), from the parent indices; null: a chain.
 __device__ __forceinline__ void build_ancestors(int tid, int b, int T, int Tq, const int32_t* parents, int* s_par, AncSet* s_anc) {
@@ -68,96 +86,123 @@ __device__ __forceinline__ uint32_t visible_word(AncSet anc, int len, int slot0)
     return ~0u;
 }
 
-// One workgroup = 16 RB rows of one (cache, KV head) x one slice of its keys.  Its four wavefronts hold the same rows and take
+// What a workgroup of either path works on.
+struct PrefixWork {
+    int rg, slice, cache, g;
+    int len, Tq, n_keys;               // Tq: nodes of the sequence (own caches only)
+    int t0, t1;                        // tiles of 64 keys
+};
+template <bool OWN>
+__device__ __forceinline__ PrefixWork prefix_work(const PrefixArgs& a, int wg) {
+    const PrefixPart& pt = a.part[OWN];
+    PrefixWork w;
+    w.rg = wg % pt.n_rg;                                   // neighbours read the same keys
+    const int ps = wg / pt.n_rg;
+    w.slice = ps % pt.n_slices;
+    const int pair = ps / pt.n_slices;
+    w.cache = pair / a.H_kv;
+    w.g = pair - w.cache * a.H_kv;
+    w.len = min(max(pt.lens[w.cache], 0), pt.max_len);
+    w.Tq = OWN ? (a.n_query ? min(max(a.n_query[w.cache], 0), a.T) : a.T) : 0;
+    w.n_keys = w.len + w.Tq;
+    const int n_tiles = (w.n_keys + kTile - 1) / kTile;
+    const int chunk = max((n_tiles + pt.n_slices - 1) / pt.n_slices, kPrefixMinTiles);
+    w.t0 = min(n_tiles, w.slice * chunk);
+    w.t1 = min(n_tiles, w.t0 + chunk);
+    return w;
+}
+
+// Row r of a (cache, KV head): its sequence, node and head, and whether it exists.
+struct PrefixRow { int b, i, h; bool valid; };
+template <bool OWN>
+__device__ __forceinline__ PrefixRow prefix_row(const PrefixArgs& a, const PrefixWork& w, int r) {
+    const PrefixPart& pt = a.part[OWN];
+    const int rc = min(r, pt.rows - 1);
+    const int bl = OWN ? 0 : a.div_TH.div(rc), in = rc - bl * a.T * a.H_g;
+    PrefixRow x;
+    x.i = a.div_Hg.div(in);
+    x.h = w.g * a.H_g + in - x.i * a.H_g;
+    x.b = w.cache * pt.per + bl;
+    x.valid = r < pt.rows && x.i < (OWN ? w.Tq : (a.n_query ? a.n_query[x.b] : a.T));
+    return x;
+}
+__device__ __forceinline__ int64_t prefix_state_row(const PrefixArgs& a, const PrefixRow& x) { return ((int64_t)x.b * a.T + x.i) * a.H + x.h; }
+
+// ---- keys path --------------------------------------------------------------------------------------------------------
+// One workgroup = 16 RB rows of one (cache, KV head) x one slice of its keys.  Its wavefronts hold the same rows and take
 // the slice's steps of 32 keys in turn, each with a softmax state of its own, merged in LDS at the end: no barrier while keys
 // are streamed.  K fragments are loaded as the matrix instruction wants them (lane: one key, 16 bytes); V rows are loaded as
 // they lie, a lane holding DV / 16 neighbouring columns of the eight keys whose probabilities it holds after S^T = K Q^T
 // (four of each block of 16), and a byte permutation per register turns them into the operand of O^T = V^T P^T: matrix
 // instruction j then sums column DV / 16 * m + j of every lane group m.  Nothing passes through LDS on the way.
-template <bool BF16, int DK, int DV, int RB>
-__global__ void __launch_bounds__(kThreads, RB == 4 ? 1 : 2) k_prefix_stream(const PrefixArgs a) {
+template <int DV>
+struct PrefixKeysCfg {
+    static constexpr int PITCH = DV + 4;
+    static constexpr int LDS = kPrefixWaves * 16 * PITCH * 4;
+};
+
+template <bool BF16, int DK, int DV, int RB, bool OWN>
+__device__ __forceinline__ void prefix_keys(const PrefixArgs& a, int wg, char* smem, PrefixTree& tree) {
     constexpr int ES = BF16 ? 2 : 4;
     constexpr int KC = DK * ES / 64;             // 64-byte chunks of a K row
     constexpr int CW = DV / 16;                  // V columns per lane
     constexpr int VW = CW * ES / 4;              // 32-bit words of them
-    constexpr int ACC_PITCH = DV + 4;
-    __shared__ AncSet s_anc[kMaxT];
-    __shared__ int s_par[kMaxT];
+    constexpr int PITCH = PrefixKeysCfg<DV>::PITCH;
     __shared__ float s_m[kPrefixWaves][16 * RB], s_z[kPrefixWaves][16 * RB];
-    __shared__ __align__(16) float s_acc[kPrefixWaves][16][ACC_PITCH];
+    float* s_acc = reinterpret_cast<float*>(smem);
 
+    const PrefixPart& pt = a.part[OWN];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int n = lane & 15, G = lane >> 4;
-    const int wg = (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3);   // every XCD gets a contiguous range of work
-    if (wg >= a.n_wg) return;
-    const int rg = wg % a.n_rg, ps = wg / a.n_rg;                              // neighbours read the same keys
-    const int slice = ps % a.n_slices, pair = ps / a.n_slices;
-    const int cache = pair / a.H_kv, g = pair - cache * a.H_kv;
-
-    const int len = min(max(a.lens[cache], 0), a.max_len);
-    const int Tq0 = a.n_query ? min(max(a.n_query[cache * a.per], 0), a.T) : a.T;     // (own caches: this sequence's)
-    const int n_keys = a.own ? len + Tq0 : len;
+    const PrefixWork w = prefix_work<OWN>(a, wg);
 
     // ---- rows
-    bool valid[RB];
-    int node[RB];
-    int64_t grow[RB];
+    PrefixRow row[RB];
     u32x4 qf[RB][KC];
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
-        const int r = (rg * RB + rb) * 16 + n;
-        const int rc = min(r, a.rows - 1);
-        const int bl = a.div_TH.div(rc), in = rc - bl * a.T * a.H_g;
-        const int i = a.div_Hg.div(in), h = in - i * a.H_g;
-        const int b = cache * a.per + bl;
-        const int Tq = a.own ? Tq0 : (a.n_query ? a.n_query[b] : a.T);
-        valid[rb] = r < a.rows && i < Tq;
-        node[rb] = i;
-        grow[rb] = ((int64_t)b * a.T + i) * a.H + g * a.H_g + h;
-        const char* qp = a.q + b * a.q_s[0] + i * a.q_s[1] + (g * a.H_g + h) * a.q_s[2] + G * 16;
+        row[rb] = prefix_row<OWN>(a, w, (w.rg * RB + rb) * 16 + n);
+        const char* qp = a.q + row[rb].b * a.q_s[0] + row[rb].i * a.q_s[1] + row[rb].h * a.q_s[2] + G * 16;
 #pragma unroll
         for (int c = 0; c < KC; ++c) qf[rb][c] = *reinterpret_cast<const u32x4*>(qp + c * 64);
-        if (!valid[rb]) {
+        if (!row[rb].valid) {
 #pragma unroll
             for (int c = 0; c < KC; ++c) qf[rb][c] = u32x4{0, 0, 0, 0};
         }
     }
-    if (a.own) build_ancestors(tid, cache, a.T, Tq0, a.parents, s_par, s_anc);
 
     // ---- this slice's steps
-    const int n_steps = (n_keys + kPrefixStep - 1) / kPrefixStep;
-    const int chunk = max((n_steps + a.n_slices - 1) / a.n_slices, a.min_steps);
-    const int t0 = slice * chunk, t1 = min(n_steps, t0 + chunk);
-    const char* kbase = a.k + cache * a.k_s[0] + g * a.k_s[1] + G * 16;
-    const char* vbase = a.v + cache * a.v_s[0] + g * a.v_s[1] + n * (CW * ES);
-    const uint32_t krow = (uint32_t)a.k_s[2], vrow = (uint32_t)a.v_s[2];
+    const int t0 = w.t0 * (kTile / kPrefixStep), t1 = min(w.t1 * (kTile / kPrefixStep), (w.n_keys + kPrefixStep - 1) / kPrefixStep);
+    const char* kbase = pt.k + w.cache * pt.k_s[0] + w.g * pt.k_s[1] + G * 16;
+    const char* vbase = pt.v + w.cache * pt.v_s[0] + w.g * pt.v_s[1] + n * (CW * ES);
+    const uint32_t krow = (uint32_t)pt.k_s[2], vrow = (uint32_t)pt.v_s[2];
 
     u32x4 kf[2][KC];
     uint32_t vf[2][4][VW];
     auto load_k = [&](int t) {
-        const char* p = kbase + (int64_t)t * kPrefixStep * a.k_s[2];
-        const int last = n_keys - 1 - t * kPrefixStep;       // rows behind the last one repeat it; their scores are masked
+        const char* p = kbase + (int64_t)t * kPrefixStep * pt.k_s[2];
+        const int last = w.n_keys - 1 - t * kPrefixStep;       // rows behind the last one repeat it; their scores are masked
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb) {
-            const char* row = p + (uint32_t)min(kb * 16 + n, last) * krow;
+            const char* r = p + (uint32_t)min(kb * 16 + n, last) * krow;
 #pragma unroll
-            for (int c = 0; c < KC; ++c) kf[kb][c] = *reinterpret_cast<const u32x4*>(row + c * 64);
+            for (int c = 0; c < KC; ++c) kf[kb][c] = *reinterpret_cast<const u32x4*>(r + c * 64);
         }
     };
     auto load_v = [&](int t) {
-        const char* p = vbase + (int64_t)t * kPrefixStep * a.v_s[2];
-        const int last = n_keys - 1 - t * kPrefixStep;
+        const char* p = vbase + (int64_t)t * kPrefixStep * pt.v_s[2];
+        const int last = w.n_keys - 1 - t * kPrefixStep;
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                const char* row = p + (uint32_t)min(kb * 16 + 4 * G + r, last) * vrow;
+                const char* at = p + (uint32_t)min(kb * 16 + 4 * G + r, last) * vrow;
                 if constexpr (VW == 4) {
-                    const u32x4 x = *reinterpret_cast<const u32x4*>(row);
+                    const u32x4 x = *reinterpret_cast<const u32x4*>(at);
 #pragma unroll
-                    for (int w = 0; w < 4; ++w) vf[kb][r][w] = x[w];
+                    for (int e = 0; e < 4; ++e) vf[kb][r][e] = x[e];
                 } else {
-                    const u32x2 x = *reinterpret_cast<const u32x2*>(row);
+                    const u32x2 x = *reinterpret_cast<const u32x2*>(at);
                     vf[kb][r][0] = x[0];
                     vf[kb][r][1] = x[1];
                 }
@@ -173,14 +218,15 @@ __global__ void __launch_bounds__(kThreads, RB == 4 ? 1 : 2) k_prefix_stream(con
 #pragma unroll
         for (int j = 0; j < CW; ++j) acc[rb][j] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    const float raise = 8.f / a.scale_log2;      // the reference maximum follows the running one at a distance of up to 2^8
-    const int full = a.own ? len : n_keys;       // keys that every row sees
+    const float raise = kPrefixRaiseLog2 / a.scale_log2;
+    const int full = OWN ? w.len : w.n_keys;       // keys that every row sees
 
     int t = t0 + wave;
     if (t < t1) {
         load_k(t);
         load_v(t);
     }
+    if constexpr (OWN) build_ancestors(tid, w.cache, a.T, w.Tq, a.parents, tree.par, tree.anc);
     for (; t < t1; t += kPrefixWaves) {
         const int next = t + kPrefixWaves;
         f32x4 s[RB][2];
@@ -197,12 +243,7 @@ __global__ void __launch_bounds__(kThreads, RB == 4 ? 1 : 2) k_prefix_stream(con
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb) {
             if ((t + 1) * kPrefixStep > full) {      // (uniform)
-                uint32_t word;
-                if (a.own) {
-                    word = visible_word(s_anc[node[rb]], len, t * kPrefixStep);
-                } else {
-                    word = (1u << (n_keys - t * kPrefixStep)) - 1u;
-                }
+                const uint32_t word = OWN ? visible_word(tree.anc[row[rb].i], w.len, t * kPrefixStep) : (1u << (w.n_keys - t * kPrefixStep)) - 1u;
 #pragma unroll
                 for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
@@ -244,9 +285,9 @@ __global__ void __launch_bounds__(kThreads, RB == 4 ? 1 : 2) k_prefix_stream(con
         for (int j = 0; j < CW; ++j) {
             if constexpr (BF16) {
                 const uint32_t sel = (j & 1) ? 0x07060302u : 0x05040100u;      // the upper or the lower halves of two keys
-                const int w = j >> 1;
-                const u32x4 vt = {__builtin_amdgcn_perm(vf[0][1][w], vf[0][0][w], sel), __builtin_amdgcn_perm(vf[0][3][w], vf[0][2][w], sel),
-                                  __builtin_amdgcn_perm(vf[1][1][w], vf[1][0][w], sel), __builtin_amdgcn_perm(vf[1][3][w], vf[1][2][w], sel)};
+                const int e = j >> 1;
+                const u32x4 vt = {__builtin_amdgcn_perm(vf[0][1][e], vf[0][0][e], sel), __builtin_amdgcn_perm(vf[0][3][e], vf[0][2][e], sel),
+                                  __builtin_amdgcn_perm(vf[1][1][e], vf[1][0][e], sel), __builtin_amdgcn_perm(vf[1][3][e], vf[1][2][e], sel)};
 #pragma unroll
                 for (int rb = 0; rb < RB; ++rb) acc[rb][j] = mma_frag<true>(vt, pk[rb][0], acc[rb][j]);
             } else {
@@ -261,12 +302,12 @@ __global__ void __launch_bounds__(kThreads, RB == 4 ? 1 : 2) k_prefix_stream(con
         if (next < t1) load_v(next);
     }
 
-    // ---- the four wavefronts' states become one
+    // ---- the wavefronts' states become one
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
         z[rb] = xor32_add(xor16_add(z[rb]));
         if (G == 0) {
-            s_m[wave][rb * 16 + n] = mref[rb] * a.scale_log2;
+            s_m[wave][rb * 16 + n] = mref[rb] * a.scale_log2;      // statistics leave the kernel in the log2 domain
             s_z[wave][rb * 16 + n] = z[rb];
         }
     }
@@ -275,36 +316,313 @@ __global__ void __launch_bounds__(kThreads, RB == 4 ? 1 : 2) k_prefix_stream(con
     for (int rb = 0; rb < RB; ++rb) {
         float M = -INFINITY, Z = 0.f;
 #pragma unroll
-        for (int w = 0; w < kPrefixWaves; ++w)
-            if (!(s_z[w][rb * 16 + n] == 0.f)) M = max_nan(M, s_m[w][rb * 16 + n]);
+        for (int o = 0; o < kPrefixWaves; ++o)
+            if (!(s_z[o][rb * 16 + n] == 0.f)) M = max_nan(M, s_m[o][rb * 16 + n]);
 #pragma unroll
-        for (int w = 0; w < kPrefixWaves; ++w)
-            if (!(s_z[w][rb * 16 + n] == 0.f)) Z += s_z[w][rb * 16 + n] * fast_exp2(s_m[w][rb * 16 + n] - M);
+        for (int o = 0; o < kPrefixWaves; ++o)
+            if (!(s_z[o][rb * 16 + n] == 0.f)) Z += s_z[o][rb * 16 + n] * fast_exp2(s_m[o][rb * 16 + n] - M);
         const float f = z[rb] == 0.f ? 0.f : fast_exp2(mref[rb] * a.scale_log2 - M);
-        const int64_t pr = (int64_t)(a.slot0 + slice) * a.rows_total + grow[rb];
-        if (wave == 0 && G == 0 && valid[rb]) *reinterpret_cast<float2*>(a.part_stats + pr * 2) = make_float2(M, Z);
+        const int64_t slot = (int64_t)(pt.slot0 + w.slice) * a.rows_total;
+        if (wave == 0 && G == 0 && row[rb].valid)
+            *reinterpret_cast<float2*>(a.part_stats + (slot + prefix_state_row(a, row[rb])) * 2) = make_float2(M, Z);
         if (t0 >= t1) continue;                      // (uniform) an empty slice leaves Z = 0 and no sums
         if (rb > 0) __syncthreads();
 #pragma unroll
         for (int r = 0; r < 4; ++r)
 #pragma unroll
             for (int j = 0; j < CW; j += 4)
-                *reinterpret_cast<f32x4*>(&s_acc[wave][n][CW * (4 * G + r) + j]) =
+                *reinterpret_cast<f32x4*>(s_acc + (wave * 16 + n) * PITCH + CW * (4 * G + r) + j) =
                     f32x4{acc[rb][j][r] * f, acc[rb][j + 1][r] * f, acc[rb][j + 2][r] * f, acc[rb][j + 3][r] * f};
         __syncthreads();
-        for (int e = tid; e < 16 * DV / 4; e += kThreads) {
-            const int row = e / (DV / 4), c = e % (DV / 4) * 4;
-            f32x4 sum = *reinterpret_cast<const f32x4*>(&s_acc[0][row][c]);
+        for (int e = tid; e < 16 * DV / 4; e += kPrefixThreads) {
+            const int rr = e / (DV / 4), c = e % (DV / 4) * 4;
+            f32x4 sum = *reinterpret_cast<const f32x4*>(s_acc + rr * PITCH + c);
 #pragma unroll
-            for (int w = 1; w < kPrefixWaves; ++w) sum += *reinterpret_cast<const f32x4*>(&s_acc[w][row][c]);
-            const int rr = (rg * RB + rb) * 16 + row;
-            if (rr < a.rows) {                       // (rows of nodes that do not exist have places too; nothing reads them)
-                const int bl = a.div_TH.div(rr), in = rr - bl * a.T * a.H_g;
-                const int i = a.div_Hg.div(in), h = in - i * a.H_g;
-                const int64_t gr = ((int64_t)(cache * a.per + bl) * a.T + i) * a.H + g * a.H_g + h;
-                *reinterpret_cast<f32x4*>(a.part_acc + ((int64_t)(a.slot0 + slice) * a.rows_total + gr) * DV + c) = sum;
+            for (int o = 1; o < kPrefixWaves; ++o) sum += *reinterpret_cast<const f32x4*>(s_acc + (o * 16 + rr) * PITCH + c);
+            const PrefixRow x = prefix_row<OWN>(a, w, (w.rg * RB + rb) * 16 + rr);
+            if (x.valid) *reinterpret_cast<f32x4*>(a.part_acc + (slot + prefix_state_row(a, x)) * DV + c) = sum;
+        }
+    }
+}
+
+// ---- rows path --------------------------------------------------------------------------------------------------------
+// One workgroup = 256 rows of one (cache, KV head) x one slice of its keys, one per CU.  K and V tiles of 64 rows go from
+// global memory straight into a ring of three LDS stages, two tiles ahead of the one in use; every wavefront multiplies its
+// 32 rows with them on the 32x32x16 matrix instruction:
+//   S^T = K Q^T in 32-key x 32-row blocks, K rows as the M dimension: a lane holds 16 keys of one row, so row maxima and sums
+//   stay in the lane except for one exchange between the lane halves, and P^T (bf16) is directly the B operand of
+//   O^T = V^T P^T, whose A operand the transposing LDS read brings.
+// A tile is a matrix phase (O of the tile before, S of this one) and a vector phase (softmax, and the loads of a later tile).
+// The eight wavefronts run in two halves one phase apart, with a barrier after every phase, so that of the two wavefronts of a
+// SIMD one feeds the matrix pipe while the other computes exponentials.  Wavefronts without a row only load.
+template <int DK, int DV>
+struct PrefixRowsCfg {
+    static constexpr int KROW = DK * 2, VROW = DV * 2;      // bytes per row
+    static constexpr int STEPS = DK / 16;                   // 16-element contraction steps of S^T = K Q^T
+    static constexpr int MB = DV / 32;                      // 32-column blocks of O^T
+    static constexpr int KT = kTile * KROW, VT = kTile * VROW;
+    static constexpr int STAGE = KT + VT;                   // one stage of the ring: K(t), then V(t)
+    static constexpr int LDS = 3 * STAGE;
+    static constexpr int ROWS = 32 * kPrefixWaves;
+};
+
+template <int DK, int DV, bool OWN>
+__device__ __forceinline__ void prefix_rows(const PrefixArgs& a, int wg, char* smem, PrefixTree& tree) {
+    using Cfg = PrefixRowsCfg<DK, DV>;
+    using KLoader = DirectRowTile<Cfg::KROW, 1, kPrefixThreads>;
+    using VLoader = DirectRowTile<Cfg::VROW, 2, kPrefixThreads>;
+    constexpr int STEPS = Cfg::STEPS, MB = Cfg::MB, KT = Cfg::KT, KROW = Cfg::KROW, VROW = Cfg::VROW, STAGE = Cfg::STAGE;
+    constexpr int KI = KLoader::ITERS, VI = VLoader::ITERS;     // load instructions per wavefront and tile
+
+    const PrefixPart& pt = a.part[OWN];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int n = lane & 31, hb = lane >> 5;
+    const PrefixWork w = prefix_work<OWN>(a, wg);
+    const int t0 = w.t0, t1 = w.t1;
+
+    // ---- tile loads: stage t = {K(t), V(t)} lives in slot (t - t0) % 3; the buffer's base moves with the tile, so that offsets
+    //      stay within it however long the cache is.  Past the slice's last tile the same instructions with an empty buffer
+    //      fetch nothing (the counted waits below need no cases).
+    const uint32_t krow = (uint32_t)pt.k_s[2], vrow = (uint32_t)pt.v_s[2];
+    const char* kbase = pt.k + w.cache * pt.k_s[0] + w.g * pt.k_s[1];
+    const char* vbase = pt.v + w.cache * pt.v_s[0] + w.g * pt.v_s[1];
+    KLoader kld;
+    VLoader vld;
+    kld.init(krow, tid);
+    vld.init(vrow, tid);
+    auto stage_of = [&](int t) { return smem + ((t - t0) % 3) * STAGE; };
+    auto prepare = [&](auto& loader, uint32_t row, int t) {       // (uniform; the last tile: rows behind the last one repeat it)
+        if (t < t1 && w.n_keys - t * kTile < kTile) loader.clamp(row, w.n_keys - t * kTile, tid);
+    };
+    auto load_k = [&](int t) {
+        prepare(kld, krow, t);
+        const u32x4 rsrc = KLoader::make_rsrc(kbase + (int64_t)(t < t1 ? t : t0) * kTile * pt.k_s[2], t < t1 ? (int64_t)kTile * krow : 0);
+#pragma unroll
+        for (int j = 0; j < KI; ++j) kld.issue_one(j, rsrc, 0u, stage_of(t), tid);
+    };
+    auto load_v = [&](int t) {
+        prepare(vld, vrow, t);
+        const u32x4 rsrc = VLoader::make_rsrc(vbase + (int64_t)(t < t1 ? t : t0) * kTile * pt.v_s[2], t < t1 ? (int64_t)kTile * vrow : 0);
+#pragma unroll
+        for (int j = 0; j < VI; ++j) vld.issue_one(j, rsrc, 0u, stage_of(t) + KT, tid);
+    };
+
+    if (t0 < t1) load_k(t0);
+
+    // ---- rows: B operands of S^T = K Q^T, row n of this wavefront's block, all contraction steps
+    const int r0 = w.rg * Cfg::ROWS + wave * 32;
+    const bool live = r0 < pt.rows;                               // (uniform) the wavefront has rows
+    const PrefixRow row = prefix_row<OWN>(a, w, r0 + n);
+    u32x4 qf[STEPS];
+    {
+        const char* qp = a.q + row.b * a.q_s[0] + row.i * a.q_s[1] + row.h * a.q_s[2] + hb * 16;
+#pragma unroll
+        for (int st = 0; st < STEPS; ++st) qf[st] = *reinterpret_cast<const u32x4*>(qp + st * 32);
+    }
+    if constexpr (OWN) build_ancestors(tid, w.cache, a.T, w.Tq, a.parents, tree.par, tree.anc);
+    const AncSet anc = OWN ? tree.anc[row.i] : AncSet{0ull, 0ull};
+    arrived(qf);
+    if (!row.valid) {
+#pragma unroll
+        for (int st = 0; st < STEPS; ++st) qf[st] = u32x4{0, 0, 0, 0};
+    }
+
+    // this lane's byte offsets into a K tile for the four contraction steps of a 128-byte group (key row n of a 32-key block,
+    // granule 2 q + hb), and into a V tile for the transposing reads of column block mb (key row 4 hb + (p >> 2) of a run of 16
+    // keys, 8-byte chunk p & 3 of the 16 columns 32 mb + 16 mh .., p = lane % 16, mh = bit 4 of the lane)
+    int koff[4], voff[MB];
+#pragma unroll
+    for (int q4 = 0; q4 < 4; ++q4) koff[q4] = n * KROW + KLoader::swizzled(n, 2 * q4 + hb) * 16;
+    {
+        const int p = lane & 15, mh = (lane >> 4) & 1, r = 4 * hb + (p >> 2);
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb) voff[mb] = r * VROW + VLoader::swizzled(r, 4 * mb + 2 * mh) * 16 + (p & 3) * 8;
+    }
+    const bool late = wave >= kPrefixWaves / 2;      // the half that runs one phase behind
+    const float raise = kPrefixRaiseLog2 / a.scale_log2;
+    const int full = (OWN ? w.len : w.n_keys) / kTile;      // tiles below it need no mask
+
+    f32x16 acc[MB];
+#pragma unroll
+    for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[mb][i] = 0.f;
+    float mref = -INFINITY, zrun = 0.f;
+    f32x16 s[2];            // scores of a tile, between its matrix phase and its vector phase
+    u32x4 pk[2][2];         // its probabilities, between the vector phase and the next matrix phase
+
+    // Between two phases.  Into the even phase of tile t: K(t) and V(t - 1) have landed (issued two tiles ago; loads complete in
+    // issue order, and only K(t + 1) and V(t) were issued since), and every wavefront has left K(t - 1) and V(t - 2), whose
+    // places K(t + 2) and V(t + 1) take.
+    auto boundary = [&](bool into_even) {
+        if (into_even) wait_vmcnt<KI + VI>();
+        __syncthreads();
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    auto issue_ahead = [&](int t) {
+        load_k(t + 2);
+        load_v(t + 1);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    // Matrix phase: O^T += V(tile - 1)^T P^T (not for the first tile), then S^T = K(tile) Q^T (not behind the last one), one
+    // stream of fragments with LEAD reads ahead of their matrix instructions.
+    //   accumulation, fragment i: 32 columns of V (block i % MB) against keys 16 (i / MB) .. + 15
+    //   products, fragment i: contraction step i / 2 of key block i % 2; lane layout of s[kb]: row n, key 32 kb + 8 j + 4 hb + r
+    //     at vector index 4 j + r
+    auto matrix_phase = [&](auto first, int tile) {
+        constexpr int N_V = decltype(first)::value ? 0 : 4 * MB, N = N_V + 2 * STEPS, LEAD = 6;
+        const char* kt = stage_of(tile);
+        const char* vt = stage_of(tile - 1 + (decltype(first)::value ? 1 : 0)) + KT;
+        auto frag = [&](int i) {
+            if (i < N_V) {
+                const int kh = i / MB, mb = i % MB;
+                const u32x2 v0 = lds_read_tr16(vt + voff[mb] + (16 * kh) * VROW);
+                const u32x2 v1 = lds_read_tr16(vt + voff[mb] + (16 * kh + 8) * VROW);
+                return u32x4{v0[0], v0[1], v1[0], v1[1]};
+            }
+            const int st = (i - N_V) >> 1, kb = (i - N_V) & 1;
+            return lds_read16(kt + kb * 32 * KROW + koff[st & 3] + (st >> 2) * 128);
+        };
+        __builtin_amdgcn_s_setprio(1);      // above the other half's vector phase, or the first LDS reads would wait for it
+        u32x4 fb[LEAD];
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < LEAD; ++i) fb[i] = frag(i);
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[kb][i] = 0.f;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            __builtin_amdgcn_sched_barrier(0);
+            if (N_V && i == N_V && tile >= t1) break;      // (uniform)
+            if (i < N_V) {
+                const int kh = i / MB, mb = i % MB;
+                acc[mb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, fb[i % LEAD]), __builtin_bit_cast(bf16x8, pk[kh >> 1][kh & 1]),
+                                                                  acc[mb], 0, 0, 0);
+            } else {
+                const int st = (i - N_V) >> 1, kb = (i - N_V) & 1;
+                s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, fb[i % LEAD]), __builtin_bit_cast(bf16x8, qf[st]), s[kb], 0, 0, 0);
+            }
+            if (i + LEAD < N) fb[i % LEAD] = frag(i + LEAD);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_setprio(0);
+    };
+    // Vector phase, in the log2 domain: scores -> bf16 probabilities (pk[kb][h] = keys 32 kb + 16 h .. + 15 in the order the products
+    // delivered them).
+    auto softmax = [&](int tile) {
+        issue_ahead(late ? tile + 1 : tile);
+        if (!live) return;
+        if (tile >= full) {       // (uniform)
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb) {
+                const int slot0 = tile * kTile + 32 * kb;
+                uint32_t word;
+                if constexpr (OWN) word = visible_word(anc, w.len, slot0);
+                else word = w.n_keys >= slot0 + 32 ? ~0u : (w.n_keys <= slot0 ? 0u : (1u << (w.n_keys - slot0)) - 1u);
+                word >>= 4 * hb;
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (!((word >> (8 * (i >> 2) + (i & 3))) & 1u)) s[kb][i] = -INFINITY;
             }
         }
+        float mx = max_nan(s[0][0], s[1][0]);
+#pragma unroll
+        for (int i = 1; i < 16; ++i) mx = max_nan(mx, max_nan(s[0][i], s[1][i]));
+        mx = xor32_max(mx);
+        const bool up = mx > mref + raise;
+        const float m_new = up ? mx : mref;
+        const float m_use = (m_new == -INFINITY) ? 0.f : m_new;
+        const float alpha = up ? fast_exp2((mref - m_use) * a.scale_log2) : 1.f;
+        const float neg_ms = -m_use * a.scale_log2;
+        float rs4[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+            float p[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                p[i] = fast_exp2(__builtin_fmaf(s[kb][i], a.scale_log2, neg_ms));
+                rs4[i & 3] += p[i];
+            }
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                bf16x8 v;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = (__bf16)p[8 * h + e];
+                pk[kb][h] = __builtin_bit_cast(u32x4, v);
+            }
+        }
+        zrun = zrun * alpha + xor32_add((rs4[0] + rs4[1]) + (rs4[2] + rs4[3]));
+        mref = m_new;
+        if (__builtin_amdgcn_ballot_w64(alpha != 1.f) != 0ull) {    // uniform; rare
+#pragma unroll
+            for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) acc[mb][i] *= alpha;
+        }
+        asm volatile("" : "+v"(pk[0][0]), "+v"(pk[0][1]), "+v"(pk[1][0]), "+v"(pk[1][1]));     // (the conversions belong to this phase)
+        __builtin_amdgcn_sched_barrier(0);
+    };
+
+    if (t0 < t1) {
+        wait_vmcnt<0>();
+        __syncthreads();
+        load_k(t0 + 1);
+        load_v(t0);
+        __builtin_amdgcn_sched_barrier(0);
+        if (late) {
+            issue_ahead(t0);
+            boundary(false);
+        }
+        if (live) matrix_phase(std::true_type{}, t0);
+        for (int tile = t0;; ++tile) {
+            boundary(late);
+            softmax(tile);
+            boundary(!late);
+            if (live) matrix_phase(std::false_type{}, tile + 1);
+            if (tile + 1 == t1) break;
+        }
+        if (!late) boundary(false);
+        wait_vmcnt<0>();        // (the empty loads count too)
+    }
+
+    // ---- partial state of this slice: (reference maximum, Z) per row and the un-normalised accumulator; lane layout of
+    //      acc[mb]: row n of the block, columns 32 mb + 8 j + 4 hb + r at vector index 4 j + r
+    if (row.valid) {
+        const int64_t pr = (int64_t)(pt.slot0 + w.slice) * a.rows_total + prefix_state_row(a, row);
+        if (hb == 0) *reinterpret_cast<float2*>(a.part_stats + pr * 2) = make_float2(mref * a.scale_log2, zrun);
+        if (!(zrun == 0.f)) {
+#pragma unroll
+            for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    *reinterpret_cast<f32x4*>(a.part_acc + pr * DV + 32 * mb + 8 * j + 4 * hb) =
+                        f32x4{acc[mb][4 * j], acc[mb][4 * j + 1], acc[mb][4 * j + 2], acc[mb][4 * j + 3]};
+        }
+    }
+}
+
+// Path of a part: 0 the rows path, 1 and 2 the keys path with 16 and 32 rows.
+template <bool BF16, int DK, int DV, int PATH, bool OWN>
+__device__ __forceinline__ void prefix_path(const PrefixArgs& a, int wg, char* smem, PrefixTree& tree) {
+    if constexpr (PATH == 0) prefix_rows<DK, DV, OWN>(a, wg, smem, tree);
+    else prefix_keys<BF16, DK, DV, PATH, OWN>(a, wg, smem, tree);
+}
+
+// The prefix's workgroups first (they are the longer ones), then those of the sequences' own keys; within each part every XCD
+// gets a contiguous range.
+template <bool BF16, int DK, int DV, int PREFIX, int OWN>
+__global__ void __launch_bounds__(kPrefixThreads, 1) __attribute__((amdgpu_waves_per_eu(2, 2))) k_prefix(const PrefixArgs a) {
+    extern __shared__ __align__(16) char smem[];
+    __shared__ PrefixTree tree;
+    const int n0 = a.part[0].n_pad;
+    if ((int)blockIdx.x < n0) {
+        const int wg = (blockIdx.x & 7) * (n0 >> 3) + (blockIdx.x >> 3);
+        if (wg < a.part[0].n_wg) prefix_path<BF16, DK, DV, PREFIX, false>(a, wg, smem, tree);
+    } else {
+        const int id = blockIdx.x - n0, wg = (id & 7) * (a.part[1].n_pad >> 3) + (id >> 3);
+        if (wg < a.part[1].n_wg) prefix_path<BF16, DK, DV, OWN, true>(a, wg, smem, tree);
     }
 }
 

@@ -3,6 +3,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 #include <cstring>
 
@@ -15,33 +16,35 @@ namespace {
 
 using namespace ssv;
 
+constexpr int kMaxDevices = 64;   // per-device one-time set-up flags
+
 int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 bool misaligned(const void* p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to != 0; }
 
 // ---- shared-prefix attention
 constexpr int kPrefixMaxSlices = 32;       // per part (prefix, own rows)
-constexpr int kPrefixWgs = 512;            // one round of workgroups: two per CU
+constexpr int kPrefixWgs = 256;            // one round of workgroups: one per CU
 
-struct PrefixPart {
-    int caches, per, rows, rb, n_rg, n_slices, n_wg;
+struct PartPlan {
+    int caches, per, rows, path, n_rg, n_slices, n_wg;
 };
 
 struct PrefixLayout {
     int H_g, es;
-    PrefixPart part[2];          // prefix (n_slices = 0: none), own rows
+    PartPlan part[2];            // prefix (n_slices = 0: none), own rows
     int n_slots;
     int64_t rows_total;
     int64_t q_s[3], out_s[3];    // bytes
     size_t off_stats, off_acc, total;
 };
 
-// Slices that fill one round of workgroups, none shorter than two steps for each of a workgroup's wavefronts.
-int plan_part(PrefixPart* pt, int H_kv, int64_t max_keys) {
-    pt->rb = pt->rows > 32 ? 4 : (pt->rows > 16 ? 2 : 1);
-    pt->n_rg = ceil_div(pt->rows, 16 * pt->rb);
+// Slices that fill one round of workgroups.
+int plan_part(PartPlan* pt, bool bf16, int H_kv, int64_t max_keys) {
+    pt->path = pt->rows <= 16 ? 1 : (bf16 ? 0 : 2);
+    pt->n_rg = ceil_div(pt->rows, pt->path ? 16 * pt->path : 256);
     const int64_t groups = (int64_t)pt->caches * H_kv * pt->n_rg;
-    const int64_t by_keys = (max_keys + 8 * kPrefixStep - 1) / (8 * kPrefixStep);
+    const int64_t by_keys = (max_keys + kPrefixMinTiles * kTile - 1) / (kPrefixMinTiles * kTile);
     pt->n_slices = (int)std::max<int64_t>(1, std::min<int64_t>({kPrefixWgs / groups, by_keys, kPrefixMaxSlices}));
     if (groups * pt->n_slices > (1 << 24)) return SSV_EUNSUPPORTED;
     pt->n_wg = (int)(groups * pt->n_slices);
@@ -65,8 +68,8 @@ int prefix_layout(const ssv_prefix_params* p, PrefixLayout* lo) {
         for (int j = 0; j < 3; ++j) {
             if (strides[s][j] < 0 || strides[s][j] * es % 16) return SSV_EINVAL;
             if (j == 2 && strides[s][j] < (s % 2 ? p->d_v : p->d_k)) return SSV_EINVAL;
-            // a step's rows are addressed by 32-bit offsets from its first one
-            if (j == 2 && strides[s][j] * es >= (1 << 26)) return SSV_EUNSUPPORTED;
+            // a tile's rows are addressed by 31-bit offsets from its first one
+            if (j == 2 && strides[s][j] * es >= (1 << 25)) return SSV_EUNSUPPORTED;
         }
     std::memset(lo, 0, sizeof(*lo));
     const int64_t* given[2] = {p->q_stride, p->out_stride};
@@ -86,18 +89,19 @@ int prefix_layout(const ssv_prefix_params* p, PrefixLayout* lo) {
     lo->es = es;
     lo->rows_total = (int64_t)p->B * p->T * p->H;
     if (lo->rows_total >= (1ll << 31)) return SSV_EUNSUPPORTED;
-    PrefixPart& shared = lo->part[0];
+    const bool bf16 = p->dtype == SSV_BF16;
+    PartPlan& shared = lo->part[0];
     if (p->max_prefix_len) {
         shared.caches = p->n_prefix;
         shared.per = p->B / p->n_prefix;
         shared.rows = shared.per * p->T * H_g;
-        if (const int rc = plan_part(&shared, p->H_kv, p->max_prefix_len)) return rc;
+        if (const int rc = plan_part(&shared, bf16, p->H_kv, p->max_prefix_len)) return rc;
     }
-    PrefixPart& own = lo->part[1];
+    PartPlan& own = lo->part[1];
     own.caches = p->B;
     own.per = 1;
     own.rows = p->T * H_g;
-    if (const int rc = plan_part(&own, p->H_kv, (int64_t)p->max_seq_len + p->T)) return rc;
+    if (const int rc = plan_part(&own, bf16, p->H_kv, (int64_t)p->max_seq_len + p->T)) return rc;
     lo->n_slots = shared.n_slices + own.n_slices;
     lo->off_stats = 0;
     lo->off_acc = align_up((size_t)lo->n_slots * lo->rows_total * 8, 256);
@@ -105,48 +109,66 @@ int prefix_layout(const ssv_prefix_params* p, PrefixLayout* lo) {
     return SSV_OK;
 }
 
+template <bool BF16, int DK, int DV, int PREFIX, int OWN>
+int prefix_enqueue(const PrefixArgs& a, hipStream_t stream) {
+    constexpr int rows = PREFIX == 0 || OWN == 0 ? PrefixRowsCfg<DK, DV>::LDS : 0;
+    constexpr int keys = PREFIX != 0 || OWN != 0 ? PrefixKeysCfg<DV>::LDS : 0;
+    constexpr int lds = rows > keys ? rows : keys;
+    const auto fn = k_prefix<BF16, DK, DV, PREFIX, OWN>;
+    if (lds > 64 * 1024) {      // once per device and kernel
+        static std::atomic<bool> raised[kMaxDevices];
+        int dev = 0;
+        if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= kMaxDevices) return SSV_ELAUNCH;
+        if (!raised[dev].load(std::memory_order_acquire)) {
+            if (hipFuncSetAttribute((const void*)fn, hipFuncAttributeMaxDynamicSharedMemorySize, lds) != hipSuccess) return SSV_ELAUNCH;
+            raised[dev].store(true, std::memory_order_release);
+        }
+    }
+    hipLaunchKernelGGL(fn, dim3(a.part[0].n_pad + a.part[1].n_pad), dim3(kPrefixThreads), lds, stream, a);
+    return hipGetLastError() == hipSuccess ? SSV_OK : SSV_ELAUNCH;
+}
+
 template <bool BF16, int DK, int DV>
 int prefix_launch(const void* q, const void* kp, const void* vp, const void* k, const void* v, const int32_t* prefix_lens,
                   const int32_t* seq_lens, const int32_t* n_query, const int32_t* parents, const ssv_prefix_params* p, void* out,
                   char* ws, const PrefixLayout& lo, hipStream_t stream) {
     const float scale = p->scale > 0.f ? p->scale : 1.f / std::sqrt((float)p->d_k);
+    PrefixArgs a{};
+    a.q = (const char*)q;
+    a.n_query = n_query;
+    a.parents = parents;
+    a.part_stats = (float*)(ws + lo.off_stats);
+    a.part_acc = (float*)(ws + lo.off_acc);
+    a.T = p->T; a.H = p->H; a.H_kv = p->H_kv; a.H_g = lo.H_g;
+    a.scale_log2 = scale * 1.4426950408889634f;
+    a.rows_total = lo.rows_total;
+    a.div_TH = FastDiv::of(p->T * lo.H_g);
+    a.div_Hg = FastDiv::of(lo.H_g);
+    for (int j = 0; j < 3; ++j) a.q_s[j] = lo.q_s[j];
     for (int own = 0; own < 2; ++own) {
-        const PrefixPart& pt = lo.part[own];
-        if (!pt.n_slices) continue;
-        PrefixArgs a{};
-        a.q = (const char*)q;
-        a.k = (const char*)(own ? k : kp);
-        a.v = (const char*)(own ? v : vp);
-        a.lens = own ? seq_lens : prefix_lens;
-        a.n_query = n_query;
-        a.parents = parents;
-        a.part_stats = (float*)(ws + lo.off_stats);
-        a.part_acc = (float*)(ws + lo.off_acc);
-        a.T = p->T; a.H = p->H; a.H_kv = p->H_kv; a.H_g = lo.H_g;
-        a.per = pt.per; a.rows = pt.rows; a.n_rg = pt.n_rg;
-        a.own = own;
-        a.max_len = own ? p->max_seq_len : p->max_prefix_len;
-        a.n_slices = pt.n_slices;
-        a.slot0 = own ? lo.part[0].n_slices : 0;
-        a.min_steps = 2 * kPrefixWaves;
-        a.n_wg = pt.n_wg;
-        a.scale_log2 = scale * 1.4426950408889634f;
-        a.rows_total = lo.rows_total;
-        a.div_TH = FastDiv::of(p->T * lo.H_g);
-        a.div_Hg = FastDiv::of(lo.H_g);
+        const PartPlan& pl = lo.part[own];
+        PrefixPart& pt = a.part[own];
+        pt.k = (const char*)(own ? k : kp);
+        pt.v = (const char*)(own ? v : vp);
+        pt.lens = own ? seq_lens : prefix_lens;
+        pt.per = pl.per; pt.rows = pl.rows; pt.n_rg = pl.n_rg;
+        pt.max_len = own ? p->max_seq_len : p->max_prefix_len;
+        pt.n_slices = pl.n_slices;
+        pt.slot0 = own ? lo.part[0].n_slices : 0;
+        pt.n_wg = pl.n_wg;
+        pt.n_pad = (int)align_up(pl.n_wg, 8);
         for (int j = 0; j < 3; ++j) {
-            a.k_s[j] = (own ? p->k_stride : p->kp_stride)[j] * lo.es;
-            a.v_s[j] = (own ? p->v_stride : p->vp_stride)[j] * lo.es;
-            a.q_s[j] = lo.q_s[j];
+            pt.k_s[j] = (own ? p->k_stride : p->kp_stride)[j] * lo.es;
+            pt.v_s[j] = (own ? p->v_stride : p->vp_stride)[j] * lo.es;
         }
-        const dim3 grid(align_up(pt.n_wg, 8));
-        switch (pt.rb) {
-            case 1: hipLaunchKernelGGL((k_prefix_stream<BF16, DK, DV, 1>), grid, dim3(kThreads), 0, stream, a); break;
-            case 2: hipLaunchKernelGGL((k_prefix_stream<BF16, DK, DV, 2>), grid, dim3(kThreads), 0, stream, a); break;
-            default: hipLaunchKernelGGL((k_prefix_stream<BF16, DK, DV, 4>), grid, dim3(kThreads), 0, stream, a); break;
-        }
-        if (hipGetLastError() != hipSuccess) return SSV_ELAUNCH;
     }
+    // the prefix's rows are the own ones of one sequence or more: its path is the same or the next one up
+    const int own = lo.part[1].path, shared = lo.part[0].n_slices ? lo.part[0].path : own;
+    constexpr int MANY = BF16 ? 0 : 2;
+    const int rc = own == MANY      ? prefix_enqueue<BF16, DK, DV, MANY, MANY>(a, stream)
+                   : shared == MANY ? prefix_enqueue<BF16, DK, DV, MANY, 1>(a, stream)
+                                    : prefix_enqueue<BF16, DK, DV, 1, 1>(a, stream);
+    if (rc != SSV_OK) return rc;
     PrefixCombineArgs c{};
     c.part_stats = (const float*)(ws + lo.off_stats);
     c.part_acc = (const float*)(ws + lo.off_acc);
