@@ -44,6 +44,7 @@ struct PrefixArgs {
 constexpr int kPrefixThreads = 512;
 constexpr int kPrefixWaves = kPrefixThreads / 64;
 constexpr int kPrefixStep = 32;        // keys per step of a wavefront on the keys path
+constexpr int kPrefixMaxSlots = 64;    // partial states per row
 constexpr int kPrefixMinTiles = 2;     // tiles of 64 keys that a slice holds at least
 constexpr float kPrefixRaiseLog2 = 8.f;   // the reference maximum follows the running one at a distance of up to 2^8
 
@@ -84,6 +85,12 @@ __device__ __forceinline__ uint32_t visible_word(AncSet anc, int len, int slot0)
     if (off > 0) return (uint32_t)((anc.lo >> off) | (anc.hi << (64 - off)));
     if (off > -32) return (uint32_t)((anc.lo << -off) | ((1ull << -off) - 1ull));
     return ~0u;
+}
+
+// sum + the two bf16 values of a register.
+__device__ __forceinline__ float add_bf16_pair(uint32_t pair, float sum) {
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pair), __builtin_bit_cast(bf16x2, 0x3f803f80u), sum, false);
 }
 
 // What a workgroup of either path works on.
@@ -380,34 +387,37 @@ __device__ __forceinline__ void prefix_rows(const PrefixArgs& a, int wg, char* s
     const PrefixWork w = prefix_work<OWN>(a, wg);
     const int t0 = w.t0, t1 = w.t1;
 
-    // ---- tile loads: stage t = {K(t), V(t)} lives in slot (t - t0) % 3; the buffer's base moves with the tile, so that offsets
-    //      stay within it however long the cache is.  Past the slice's last tile the same instructions with an empty buffer
-    //      fetch nothing (the counted waits below need no cases).
+    // ---- tile loads: K(t), then V(t), in one of three stages of the ring that take turns.  A load moves its pointer on, so that
+    //      offsets stay within a tile however long the cache is; past the slice's last tile it is the same instructions with
+    //      an empty buffer, which fetch nothing (the counted waits below need no cases).
     const uint32_t krow = (uint32_t)pt.k_s[2], vrow = (uint32_t)pt.v_s[2];
-    const char* kbase = pt.k + w.cache * pt.k_s[0] + w.g * pt.k_s[1];
-    const char* vbase = pt.v + w.cache * pt.v_s[0] + w.g * pt.v_s[1];
+    const int64_t kstep = pt.k_s[2] * kTile, vstep = pt.v_s[2] * kTile;
+    const char* knext = pt.k + w.cache * pt.k_s[0] + w.g * pt.k_s[1] + t0 * kstep;      // of the next tile to load
+    const char* vnext = pt.v + w.cache * pt.v_s[0] + w.g * pt.v_s[1] + t0 * vstep;
+    int kleft = w.n_keys - t0 * kTile, vleft = kleft;             // rows from there on
+    int kt_left = t1 - t0, vt_left = t1 - t0;                     // tiles of the slice from there on
     KLoader kld;
     VLoader vld;
     kld.init(krow, tid);
     vld.init(vrow, tid);
-    auto stage_of = [&](int t) { return smem + ((t - t0) % 3) * STAGE; };
-    auto prepare = [&](auto& loader, uint32_t row, int t) {       // (uniform; the last tile: rows behind the last one repeat it)
-        if (t < t1 && w.n_keys - t * kTile < kTile) loader.clamp(row, w.n_keys - t * kTile, tid);
-    };
-    auto load_k = [&](int t) {
-        prepare(kld, krow, t);
-        const u32x4 rsrc = KLoader::make_rsrc(kbase + (int64_t)(t < t1 ? t : t0) * kTile * pt.k_s[2], t < t1 ? (int64_t)kTile * krow : 0);
+    const uint32_t lds0 = __builtin_amdgcn_readfirstlane(lds_addr(smem));
+    const uint32_t kdst = lds0 + wave * (KI * 1024), vdst = lds0 + KT + wave * (VI * 1024);
+    uint32_t kstage = 0, vstage = 0;                              // offsets of the stages that the next loads fill
+    auto load = [&](auto& loader, const char*& next, int64_t step, uint32_t row, int& left, int& tiles, uint32_t dst, uint32_t& stage) {
+        using Loader = std::remove_reference_t<decltype(loader)>;
+        if (tiles > 0 && left < kTile) loader.clamp(row, left, tid);      // (uniform; the last tile: rows behind the last one repeat it)
+        const uint64_t at = (uint64_t)next;
+        const u32x4 rsrc = {(uint32_t)at, (uint32_t)(at >> 32) & 0xffffu, tiles > 0 ? (uint32_t)step : 0u, 0x00020000u};
 #pragma unroll
-        for (int j = 0; j < KI; ++j) kld.issue_one(j, rsrc, 0u, stage_of(t), tid);
+        for (int j = 0; j < Loader::ITERS; ++j) buffer_load_lds16(rsrc, dst + stage + j * 1024, loader.off[j], 0u);
+        next += step;
+        left -= kTile;
+        --tiles;
+        stage = stage == 2 * STAGE ? 0u : stage + STAGE;
     };
-    auto load_v = [&](int t) {
-        prepare(vld, vrow, t);
-        const u32x4 rsrc = VLoader::make_rsrc(vbase + (int64_t)(t < t1 ? t : t0) * kTile * pt.v_s[2], t < t1 ? (int64_t)kTile * vrow : 0);
-#pragma unroll
-        for (int j = 0; j < VI; ++j) vld.issue_one(j, rsrc, 0u, stage_of(t) + KT, tid);
-    };
-
-    if (t0 < t1) load_k(t0);
+    auto load_k = [&] { load(kld, knext, kstep, krow, kleft, kt_left, kdst, kstage); };
+    auto load_v = [&] { load(vld, vnext, vstep, vrow, vleft, vt_left, vdst, vstage); };
+    if (t0 < t1) load_k();
 
     // ---- rows: B operands of S^T = K Q^T, row n of this wavefront's block, all contraction steps
     const int r0 = w.rg * Cfg::ROWS + wave * 32;
@@ -439,7 +449,6 @@ __device__ __forceinline__ void prefix_rows(const PrefixArgs& a, int wg, char* s
         for (int mb = 0; mb < MB; ++mb) voff[mb] = r * VROW + VLoader::swizzled(r, 4 * mb + 2 * mh) * 16 + (p & 3) * 8;
     }
     const bool late = wave >= kPrefixWaves / 2;      // the half that runs one phase behind
-    const float raise = kPrefixRaiseLog2 / a.scale_log2;
     const int full = (OWN ? w.len : w.n_keys) / kTile;      // tiles below it need no mask
 
     f32x16 acc[MB];
@@ -447,7 +456,8 @@ __device__ __forceinline__ void prefix_rows(const PrefixArgs& a, int wg, char* s
     for (int mb = 0; mb < MB; ++mb)
 #pragma unroll
         for (int i = 0; i < 16; ++i) acc[mb][i] = 0.f;
-    float mref = -INFINITY, zrun = 0.f;
+    float mref = -INFINITY, neg = 0.f, zrun = 0.f;      // reference maximum, - mref * scale, this lane's part of Z
+    float limit = -1.f;     // of a tile's sum in this lane; below 0: the row has no reference yet
     f32x16 s[2];            // scores of a tile, between its matrix phase and its vector phase
     u32x4 pk[2][2];         // its probabilities, between the vector phase and the next matrix phase
 
@@ -459,9 +469,9 @@ __device__ __forceinline__ void prefix_rows(const PrefixArgs& a, int wg, char* s
         __syncthreads();
         __builtin_amdgcn_sched_barrier(0);
     };
-    auto issue_ahead = [&](int t) {
-        load_k(t + 2);
-        load_v(t + 1);
+    auto issue_ahead = [&] {
+        load_k();
+        load_v();
         __builtin_amdgcn_sched_barrier(0);
     };
     // Matrix phase: O^T += V(tile - 1)^T P^T (not for the first tile), then S^T = K(tile) Q^T (not behind the last one), one
@@ -469,10 +479,10 @@ __device__ __forceinline__ void prefix_rows(const PrefixArgs& a, int wg, char* s
     //   accumulation, fragment i: 32 columns of V (block i % MB) against keys 16 (i / MB) .. + 15
     //   products, fragment i: contraction step i / 2 of key block i % 2; lane layout of s[kb]: row n, key 32 kb + 8 j + 4 hb + r
     //     at vector index 4 j + r
+    const char* kt = smem;              // stage of the tile whose products come next
+    const char* vt = smem + KT;         // of the tile before it
     auto matrix_phase = [&](auto first, int tile) {
         constexpr int N_V = decltype(first)::value ? 0 : 4 * MB, N = N_V + 2 * STEPS, LEAD = 6;
-        const char* kt = stage_of(tile);
-        const char* vt = stage_of(tile - 1 + (decltype(first)::value ? 1 : 0)) + KT;
         auto frag = [&](int i) {
             if (i < N_V) {
                 const int kh = i / MB, mb = i % MB;
@@ -508,11 +518,15 @@ __device__ __forceinline__ void prefix_rows(const PrefixArgs& a, int wg, char* s
         }
         __builtin_amdgcn_sched_barrier(0);
         __builtin_amdgcn_s_setprio(0);
+        vt = kt + KT;
+        kt = kt == smem + 2 * STAGE ? smem : kt + STAGE;
     };
     // Vector phase, in the log2 domain: scores -> bf16 probabilities (pk[kb][h] = keys 32 kb + 16 h .. + 15 in the order the products
-    // delivered them).
+    // delivered them).  Taken against the reference of the tiles before, without looking for a maximum: scores that exceed it show
+    // in the sum (a sum above 2^9, infinite or not a number), and only then the reference is raised and the tile taken again.
+    // Z sums the probabilities as they are rounded, so that their errors cancel in the quotient.
     auto softmax = [&](int tile) {
-        issue_ahead(late ? tile + 1 : tile);
+        issue_ahead();
         if (!live) return;
         if (tile >= full) {       // (uniform)
 #pragma unroll
@@ -527,40 +541,43 @@ __device__ __forceinline__ void prefix_rows(const PrefixArgs& a, int wg, char* s
                     if (!((word >> (8 * (i >> 2) + (i & 3))) & 1u)) s[kb][i] = -INFINITY;
             }
         }
-        float mx = max_nan(s[0][0], s[1][0]);
+        float rs4[4];
+        auto probabilities = [&] {
 #pragma unroll
-        for (int i = 1; i < 16; ++i) mx = max_nan(mx, max_nan(s[0][i], s[1][i]));
-        mx = xor32_max(mx);
-        const bool up = mx > mref + raise;
-        const float m_new = up ? mx : mref;
-        const float m_use = (m_new == -INFINITY) ? 0.f : m_new;
-        const float alpha = up ? fast_exp2((mref - m_use) * a.scale_log2) : 1.f;
-        const float neg_ms = -m_use * a.scale_log2;
-        float rs4[4] = {0.f, 0.f, 0.f, 0.f};
+            for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb) {
-            float p[16];
+                for (int h = 0; h < 2; ++h) {
+                    bf16x8 v;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                p[i] = fast_exp2(__builtin_fmaf(s[kb][i], a.scale_log2, neg_ms));
-                rs4[i & 3] += p[i];
-            }
+                    for (int e = 0; e < 8; ++e) v[e] = (__bf16)fast_exp2(__builtin_fmaf(s[kb][8 * h + e], a.scale_log2, neg));
+                    pk[kb][h] = __builtin_bit_cast(u32x4, v);
+                    float sum = 0.f;
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                bf16x8 v;
+                    for (int e = 0; e < 4; ++e) sum = add_bf16_pair(pk[kb][h][e], sum);
+                    rs4[2 * kb + h] = sum;
+                }
+        };
+        probabilities();
+        float rs = (rs4[0] + rs4[1]) + (rs4[2] + rs4[3]);
+        if (__builtin_amdgcn_ballot_w64(!(rs <= limit)) != 0ull) {       // (uniform; the first tile, rare after it)
+            float mx = s[0][0];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = (__bf16)p[8 * h + e];
-                pk[kb][h] = __builtin_bit_cast(u32x4, v);
-            }
-        }
-        zrun = zrun * alpha + xor32_add((rs4[0] + rs4[1]) + (rs4[2] + rs4[3]));
-        mref = m_new;
-        if (__builtin_amdgcn_ballot_w64(alpha != 1.f) != 0ull) {    // uniform; rare
+            for (int i = 1; i < 32; ++i) mx = max_nan(mx, s[i >> 4][i & 15]);
+            mx = xor32_max(mx);
+            const bool up = !(mx <= mref);
+            const float alpha = up && mref != -INFINITY ? fast_exp2((mref - mx) * a.scale_log2) : 1.f;
+            mref = up ? mx : mref;
+            neg = mref == -INFINITY ? 0.f : -mref * a.scale_log2;
+            limit = mref == -INFINITY ? -1.f : 512.f;
+            zrun *= alpha;
 #pragma unroll
             for (int mb = 0; mb < MB; ++mb)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) acc[mb][i] *= alpha;
+            probabilities();
+            rs = (rs4[0] + rs4[1]) + (rs4[2] + rs4[3]);
         }
+        zrun += rs;
         asm volatile("" : "+v"(pk[0][0]), "+v"(pk[0][1]), "+v"(pk[1][0]), "+v"(pk[1][1]));     // (the conversions belong to this phase)
         __builtin_amdgcn_sched_barrier(0);
     };
@@ -568,11 +585,11 @@ __device__ __forceinline__ void prefix_rows(const PrefixArgs& a, int wg, char* s
     if (t0 < t1) {
         wait_vmcnt<0>();
         __syncthreads();
-        load_k(t0 + 1);
-        load_v(t0);
+        load_k();
+        load_v();
         __builtin_amdgcn_sched_barrier(0);
         if (late) {
-            issue_ahead(t0);
+            issue_ahead();
             boundary(false);
         }
         if (live) matrix_phase(std::true_type{}, t0);
@@ -586,6 +603,7 @@ __device__ __forceinline__ void prefix_rows(const PrefixArgs& a, int wg, char* s
         if (!late) boundary(false);
         wait_vmcnt<0>();        // (the empty loads count too)
     }
+    zrun = xor32_add(zrun);
 
     // ---- partial state of this slice: (reference maximum, Z) per row and the un-normalised accumulator; lane layout of
     //      acc[mb]: row n of the block, columns 32 mb + 8 j + 4 hb + r at vector index 4 j + r
@@ -636,32 +654,61 @@ struct PrefixCombineArgs {
     int64_t out_s[3];     // bytes: sequence, node, head
 };
 
-// out = sum_s 2^(m_s - M) acc_s / sum_s 2^(m_s - M) Z_s over the slices that saw a key; DV / 4 threads per row.
+// out = sum_s 2^(m_s - M) acc_s / sum_s 2^(m_s - M) Z_s over the slices that saw a key; DV / 4 threads per row.  The small calls
+// are bound by latency: a lane of the row's group fetches the statistics of its own slots while the first eight slots' sums are
+// on their way, the maximum and the total go through lane exchanges, and every later batch of eight is fetched at once.
 template <bool BF16, int DV>
 __global__ void __launch_bounds__(kThreads) k_prefix_combine(const PrefixCombineArgs a) {
-    constexpr int TPR = DV / 4, RPW = kThreads / TPR;
+    touch_args<PrefixCombineArgs>();
+    constexpr int TPR = DV / 4, RPW = kThreads / TPR, PER = kPrefixMaxSlots / TPR, BATCH = 8;
     const int64_t row = (int64_t)blockIdx.x * RPW + threadIdx.x / TPR;
     if (row >= a.rows_total) return;
-    const int c = threadIdx.x % TPR;
+    const int l = threadIdx.x % TPR, c = l;
     const int bi = a.div_H.div((int)row), b = a.div_T.div(bi), i = bi - b * a.T, h = (int)row - bi * a.H;
     const int Tq = a.n_query ? a.n_query[b] : a.T;
-    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-    if (i < Tq) {
-        float M = -INFINITY, Z = 0.f;
-        for (int s = 0; s < a.n_slots; ++s) {
-            const float2 st = *reinterpret_cast<const float2*>(a.part_stats + ((int64_t)s * a.rows_total + row) * 2);
-            if (!(st.y == 0.f)) M = max_nan(M, st.x);
-        }
-        for (int s = 0; s < a.n_slots; ++s) {
-            const int64_t pr = (int64_t)s * a.rows_total + row;
-            const float2 st = *reinterpret_cast<const float2*>(a.part_stats + pr * 2);
-            if (st.y == 0.f) continue;
-            const float w = fast_exp2(st.x - M);
-            Z += st.y * w;
-            acc += w * *reinterpret_cast<const f32x4*>(a.part_acc + pr * DV + c * 4);
-        }
-        acc *= 1.f / Z;        // (a node sees itself: Z > 0)
+    float2 st[PER];
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+        st[k] = make_float2(0.f, 0.f);
+        if (l + k * TPR < a.n_slots) st[k] = *reinterpret_cast<const float2*>(a.part_stats + ((int64_t)(l + k * TPR) * a.rows_total + row) * 2);
     }
+    const float* at = a.part_acc + row * DV + c * 4;
+    const int64_t step = a.rows_total * DV;
+    f32x4 v[BATCH];
+#pragma unroll
+    for (int s = 0; s < BATCH; ++s) v[s] = *reinterpret_cast<const f32x4*>(at + min(s, a.n_slots - 1) * step);
+    float M = -INFINITY, Z = 0.f;
+#pragma unroll
+    for (int k = 0; k < PER; ++k)
+        if (!(st[k].y == 0.f)) M = max_nan(M, st[k].x);
+#pragma unroll
+    for (int off = 1; off < TPR; off <<= 1) M = max_nan(M, __shfl_xor(M, off, TPR));
+    float w[PER];
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+        w[k] = st[k].y == 0.f ? 0.f : fast_exp2(st[k].x - M);
+        Z += w[k] == 0.f ? 0.f : w[k] * st[k].y;
+    }
+#pragma unroll
+    for (int off = 1; off < TPR; off <<= 1) Z += __shfl_xor(Z, off, TPR);
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int k = 0; k < PER; ++k)
+        for (int s0 = k * TPR; s0 < (k + 1) * TPR && s0 < a.n_slots; s0 += BATCH) {
+            if (s0) {
+#pragma unroll
+                for (int s = 0; s < BATCH; ++s) v[s] = *reinterpret_cast<const f32x4*>(at + min(s0 + s, a.n_slots - 1) * step);
+            }
+#pragma unroll
+            for (int s = 0; s < BATCH; ++s) {
+                // (slots that saw no key, or that do not exist, hold anything: their weight is 0)
+                const float ws = __shfl(w[k], s0 - k * TPR + s, TPR);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[e] += ws == 0.f ? 0.f : ws * v[s][e];
+            }
+        }
+    acc *= 1.f / Z;
+    if (i >= Tq) acc = f32x4{0.f, 0.f, 0.f, 0.f};       // (a node that exists sees itself: Z > 0)
     char* o = a.out + b * a.out_s[0] + i * a.out_s[1] + h * a.out_s[2];
     if constexpr (BF16) {
         __bf16 r[4];

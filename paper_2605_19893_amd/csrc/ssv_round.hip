@@ -23,7 +23,7 @@ size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 bool misaligned(const void* p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to != 0; }
 
 // ---- shared-prefix attention
-constexpr int kPrefixMaxSlices = 32;       // per part (prefix, own rows)
+constexpr int kPrefixMaxSlices = kPrefixMaxSlots / 2;      // per part (prefix, own rows)
 constexpr int kPrefixWgs = 256;            // one round of workgroups: one per CU
 
 struct PartPlan {
@@ -39,16 +39,73 @@ struct PrefixLayout {
     size_t off_stats, off_acc, total;
 };
 
-// Slices that fill one round of workgroups.
-int plan_part(PartPlan* pt, bool bf16, int H_kv, int64_t max_keys) {
+// Path and row groups of a part.
+int plan_rows(PartPlan* pt, bool bf16, int H_kv) {
     pt->path = pt->rows <= 16 ? 1 : (bf16 ? 0 : 2);
     pt->n_rg = ceil_div(pt->rows, pt->path ? 16 * pt->path : 256);
-    const int64_t groups = (int64_t)pt->caches * H_kv * pt->n_rg;
-    const int64_t by_keys = (max_keys + kPrefixMinTiles * kTile - 1) / (kPrefixMinTiles * kTile);
-    pt->n_slices = (int)std::max<int64_t>(1, std::min<int64_t>({kPrefixWgs / groups, by_keys, kPrefixMaxSlices}));
-    if (groups * pt->n_slices > (1 << 24)) return SSV_EUNSUPPORTED;
-    pt->n_wg = (int)(groups * pt->n_slices);
-    return SSV_OK;
+    return (int64_t)pt->caches * H_kv * pt->n_rg * kPrefixMaxSlices > (1 << 24) ? SSV_EUNSUPPORTED : SSV_OK;
+}
+
+// What a part would cost in n slices: workgroups, and microseconds of one.  A rough model, measured at full load: a tile takes a
+// workgroup of the rows path 52 ns per matrix instruction of a wavefront (with at most four wavefronts, one per SIMD, two thirds
+// of it), one of the keys path its bytes at 80 GB/s (fp32: its products); every workgroup 7 us from its first instruction to its first tile and
+// from its last one to its end.
+struct SliceCost { int n, wgs; float us; };
+struct PartCost {
+    float tile_us;
+    int tiles, groups;
+    PartCost(const PartPlan& pt, const ssv_prefix_params* p, int64_t max_keys, float share) {
+        const float mma = (p->d_k + p->d_v) / 8.f, bytes = 64.f * (p->d_k + p->d_v) * (p->dtype == SSV_BF16 ? 2 : 4);
+        tile_us = share * (pt.path == 0 ? 0.052f * mma * (pt.rows > 128 ? 1.f : 0.67f) : (p->dtype == SSV_BF16 ? bytes / 80e3f : pt.path * 0.9f));
+        tiles = (int)((max_keys + kTile - 1) / kTile);
+        groups = pt.caches * p->H_kv * pt.n_rg;
+    }
+    SliceCost at(int n) const {
+        const int chunk = std::max(kPrefixMinTiles, (tiles + n - 1) / n);
+        return SliceCost{(tiles + chunk - 1) / chunk, groups * ((tiles + chunk - 1) / chunk), 7.f + chunk * tile_us};
+    }
+};
+
+// Slices of both parts: the pair with the least estimated time for one launch (the prefix's workgroups in rounds of 256, the own
+// ones in the places they leave) and for the partial states, which are written and read back at 4 TB/s.
+void plan_slices(PrefixLayout* lo, const ssv_prefix_params* p) {
+    static constexpr int counts[] = {1, 2, 3, 4, 5, 6, 7, 8, 10, 12, 14, 16, 20, 24, 28, 32};
+    constexpr int N = sizeof(counts) / sizeof(counts[0]);
+    const bool shared = p->max_prefix_len > 0;
+    SliceCost own[N], first = {0, 0, 0.f};
+    const PartCost oc(lo->part[1], p, (int64_t)p->max_seq_len + p->T, 0.75f);       // (sequences of mixed lengths, the bound is the longest's)
+    int n_own = 0;
+    for (int n : counts) {
+        const SliceCost c = oc.at(n);
+        if (!n_own || c.n != own[n_own - 1].n) own[n_own++] = c;
+    }
+    const float slot_us = (float)lo->rows_total * (p->d_v * 4 + 8) * 2 / 4e6f;
+    float best = 1e30f;
+    int last = -1;
+    for (int i = 0; i < (shared ? N : 1); ++i) {
+        if (shared) first = PartCost(lo->part[0], p, p->max_prefix_len, 1.f).at(counts[i]);
+        if (first.n == last) continue;
+        last = first.n;
+        const int full = first.wgs / kPrefixWgs, rest = first.wgs % kPrefixWgs, idle = kPrefixWgs - rest;
+        for (int j = 0; j < n_own; ++j) {
+            const SliceCost& c = own[j];
+            const float done = (full + (rest ? 1 : 0)) * first.us;
+            // the own workgroups fit beside the last round, or wait for it, or use its idle places alone
+            const int beside = rest ? idle * (int)(first.us / c.us) : 0;
+            float us = done;
+            if (c.wgs > beside)
+                us = std::min(done + (c.wgs - beside + kPrefixWgs - 1) / kPrefixWgs * c.us,
+                              std::max(done, full * first.us + (c.wgs + idle - 1) / idle * c.us));
+            us += (first.n + c.n) * slot_us;
+            if (us < best) {
+                best = us;
+                lo->part[0].n_slices = first.n;
+                lo->part[0].n_wg = first.wgs;
+                lo->part[1].n_slices = c.n;
+                lo->part[1].n_wg = c.wgs;
+            }
+        }
+    }
 }
 
 int prefix_layout(const ssv_prefix_params* p, PrefixLayout* lo) {
@@ -95,13 +152,14 @@ int prefix_layout(const ssv_prefix_params* p, PrefixLayout* lo) {
         shared.caches = p->n_prefix;
         shared.per = p->B / p->n_prefix;
         shared.rows = shared.per * p->T * H_g;
-        if (const int rc = plan_part(&shared, bf16, p->H_kv, p->max_prefix_len)) return rc;
+        if (const int rc = plan_rows(&shared, bf16, p->H_kv)) return rc;
     }
     PartPlan& own = lo->part[1];
     own.caches = p->B;
     own.per = 1;
     own.rows = p->T * H_g;
-    if (const int rc = plan_part(&own, bf16, p->H_kv, (int64_t)p->max_seq_len + p->T)) return rc;
+    if (const int rc = plan_rows(&own, bf16, p->H_kv)) return rc;
+    plan_slices(lo, p);
     lo->n_slots = shared.n_slices + own.n_slices;
     lo->off_stats = 0;
     lo->off_acc = align_up((size_t)lo->n_slots * lo->rows_total * 8, 256);
