@@ -81,7 +81,7 @@ typedef struct ssv_sample_params {
  *   n_query [B] or NULL: logits of nodes i >= n_query[b] are not read.
  *   tokens [B,T] int32, probs [B,T] float32 or NULL (device, written): -1 and 0 for nodes i >= n_query[b] and for nodes
  *   without a logit above -inf.
- *   workspace: >= ssv_sample_workspace_bytes(p) bytes, 256-byte aligned (NULL if that is 0); as in ssv_prefix_verify.
+ *   workspace: >= ssv_sample_workspace_bytes(p) bytes, 256-byte aligned, as in ssv_prefix_verify.
  * Weights and their sums are computed in 64 bits: a token of a large vocabulary has a weight far below the rounding of a 32-bit
  * sum, and a rounding of the running sum moves every border behind it.
  */
@@ -89,7 +89,7 @@ int ssv_sample(const void* logits, const float* temperature, const int32_t* top_
                const float* u, const int32_t* n_query, const ssv_sample_params* p, int32_t* tokens, float* probs,
                void* workspace, size_t workspace_bytes, void* stream);
 
-/* Scratch bytes ssv_sample needs for p; 0 if it needs none or p is invalid. */
+/* Scratch bytes ssv_sample needs for p; 0 if p is invalid. */
 size_t ssv_sample_workspace_bytes(const ssv_sample_params* p);
 
 /*

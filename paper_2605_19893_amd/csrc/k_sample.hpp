@@ -2,13 +2,21 @@
 // of the cumulative weights in index order.
 //
 // All three filters keep a head of the order (logit descending, index ascending), so what they keep together is
-//   { key > tau } and the first `quota` indices (ascending) of { key == tau },
-// key being the logit's bits in an order-preserving integer form.  tau of top-k is a radix selection by counts, tau of top-p
-// one by mass; masses are summed as 64-bit fixed point, so the sums do not depend on the order of the atomics.
+//   { key > tau } and, of { key == tau }, the indices up to `cut`,
+// key being the logit's bits in an order-preserving integer form.
+//
+// Two launches.  k_sample_blocks reads the logits once, 2048 per wavefront over the whole chip, and leaves per block of 2048 the
+// maximum and (where the whole vocabulary counts) the sum of weights against it, and per chunk of 8 the upper half of the
+// maximum's key.  k_sample_pick, one workgroup per row, finds the token from these: without filters by the block in which the
+// running sum passes u, of which alone the logits are read again; with filters from a list of candidates, the logits above a bound that no
+// kept entry can lie below, sorted in LDS.  Rows whose filters keep more than the list holds take the general way, radix
+// selections over the row.
 #pragma once
 #include "device_common.hpp"
 
 namespace ssv {
+
+struct SampleBlock { double sum, max; };     // of 2048 logits: sum of 2^((x - max) log2(e) / t), maximum
 
 struct SampleArgs {
     const char* logits;
@@ -16,14 +24,22 @@ struct SampleArgs {
     const int32_t *top_k, *n_query;
     int32_t* tokens;
     float* probs;
-    int T, V;
+    SampleBlock* blocks;   // [row][n_blocks]
+    uint16_t* maxima;      // [row][n_blocks * 256]: upper half of the order key of each chunk's maximum
+    int T, V, n_blocks;
+    int wg_per_row;        // k_sample_blocks
     int64_t s[2];          // bytes: sequence, node
     double mass_scale;     // fixed-point units of a weight of 1: V times it stays below 2^63
 };
 
 constexpr int kSampleThreads = 1024, kSampleWaves = kSampleThreads / 64;
 constexpr int kSampleMaxV = 1 << 20;
-constexpr int kSampleMaxIters = kSampleMaxV / (8 * kSampleThreads) + 1;     // (an unaligned row starts inside its first chunk)
+constexpr int kSampleBlock = 2048, kSampleChunks = kSampleBlock / 8;
+constexpr int kSampleMaxBlocks = kSampleMaxV / kSampleBlock + 1;            // (an unaligned row starts inside its first chunk)
+constexpr int kSampleMaxIters = kSampleMaxV / (8 * kSampleThreads) + 1;
+constexpr int kSampleList = 2048;                                           // candidates that k_sample_pick sorts
+
+__host__ __device__ __forceinline__ int sample_blocks(int V) { return (V + 7 + kSampleBlock - 1) / kSampleBlock; }
 
 __device__ __forceinline__ uint32_t order_key(float x) {
     const uint32_t b = __float_as_uint(x);
@@ -31,17 +47,112 @@ __device__ __forceinline__ uint32_t order_key(float x) {
 }
 __device__ __forceinline__ float key_value(uint32_t k) { return __uint_as_float(k ^ ((k >> 31) ? 0x80000000u : 0xffffffffu)); }
 
-// Weight of a logit; 1 at the maximum, whatever that is.
+// 2^y for y <= 0 (lower than -1100, -inf and NaN count as -1100, which gives 0): 2^n times the polynomial of degree 10 that takes the values of
+// 2^f at the eleven Chebyshev points of [-1/2, 1/2], off by at most 4e-16.  Eighteen instructions at the rate of 32-bit ones.
+__device__ __forceinline__ double exp2_64(double y) {
+    y = fmax(y, -1100.0);
+    const double n = __builtin_rint(y), f = y - n;
+    double p = 7.072585949269223e-09;
+    p = __builtin_fma(p, f, 1.0208690299958306e-07);
+    p = __builtin_fma(p, f, 1.321544258792169e-06);
+    p = __builtin_fma(p, f, 1.5252657260200837e-05);
+    p = __builtin_fma(p, f, 0.0001540353044173605);
+    p = __builtin_fma(p, f, 0.0013333558230164974);
+    p = __builtin_fma(p, f, 0.009618129107606888);
+    p = __builtin_fma(p, f, 0.05550410866444772);
+    p = __builtin_fma(p, f, 0.24022650695910097);
+    p = __builtin_fma(p, f, 0.69314718055995);
+    p = __builtin_fma(p, f, 1.0);
+    return __builtin_ldexp(p, (int)n);
+}
+
+// Weight of a logit against a maximum; 1 at the maximum, whatever that is.
 struct SampleWeight {
-    double M, inv_t;
+    double M, c;       // c = log2(e) / temperature
     float Mf;
-    __device__ __forceinline__ double operator()(float x) const {
-        if (x == Mf) return 1.0;
-        if (x == -INFINITY) return 0.0;
-        return exp(((double)x - M) * inv_t);
+    __device__ __forceinline__ double operator()(float x) const { return x == Mf ? 1.0 : exp2_64(((double)x - M) * c); }
+};
+
+// The settings of a sequence as the header reads them.
+struct SampleRule {
+    float t, top_p, min_p;
+    int top_k;
+    double c;
+    bool first;            // the first entry alone
+    bool by_k, by_p, by_m;
+    __device__ __forceinline__ bool sums() const { return !first && (by_p ? !by_k : !(by_k || by_m)); }      // the whole vocabulary's sum counts
+    __device__ __forceinline__ bool filters() const { return !first && (by_k || by_p || by_m); }
+};
+__device__ __forceinline__ SampleRule sample_rule(const SampleArgs& a, int b) {
+    SampleRule r;
+    r.t = a.temperature ? a.temperature[b] : 1.f;
+    r.top_k = a.top_k ? a.top_k[b] : 0;
+    r.top_p = a.top_p ? a.top_p[b] : 1.f;
+    r.min_p = a.min_p ? a.min_p[b] : 0.f;
+    r.first = !(r.t > 0.f) || r.top_p <= 0.f || r.top_k == 1;
+    r.by_k = r.top_k > 0 && r.top_k < a.V;
+    r.by_p = r.top_p < 1.f;
+    r.by_m = r.min_p > 0.f;
+    r.c = 1.4426950408889634 / (double)r.t;
+    return r;
+}
+
+// A row of logits in chunks of 8 from a 16-byte boundary on: chunk c holds elements 8 c - shift .. + 7.  Elements outside the
+// row read as -inf, NaN counts as -inf, -0 as 0.
+template <bool BF16>
+struct SampleRow {
+    static constexpr int ES = BF16 ? 2 : 4;
+    const char* base;
+    int V, shift, n_chunks;
+    __device__ __forceinline__ SampleRow(const SampleArgs& a, int b, int i) : base(a.logits + b * a.s[0] + i * a.s[1]), V(a.V) {
+        shift = (int)((uintptr_t)base & 15) / ES;
+        n_chunks = (V + shift + 7) / 8;
+    }
+    __device__ __forceinline__ int first(int c) const { return 8 * c - shift; }
+    __device__ __forceinline__ static float clean(float x) { return fmaxf(x + 0.f, -INFINITY); }
+    __device__ __forceinline__ void load(int c, float (&x)[8]) const {
+        const int e0 = first(c);
+        if (e0 >= 0 && e0 + 8 <= V) {
+            const u32x4* p = reinterpret_cast<const u32x4*>(base + (int64_t)e0 * ES);
+            if constexpr (BF16) {
+                const u32x4 v = *p;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    x[2 * j] = __uint_as_float(v[j] << 16);
+                    x[2 * j + 1] = __uint_as_float(v[j] & 0xffff0000u);
+                }
+            } else {
+                const u32x4 v = p[0], w = p[1];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    x[j] = __uint_as_float(v[j]);
+                    x[4 + j] = __uint_as_float(w[j]);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                x[j] = -INFINITY;
+                if (c < n_chunks && e0 + j >= 0 && e0 + j < V) {
+                    if constexpr (BF16) x[j] = __uint_as_float((uint32_t)reinterpret_cast<const uint16_t*>(base)[e0 + j] << 16);
+                    else x[j] = reinterpret_cast<const float*>(base)[e0 + j];
+                }
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = clean(x[j]);
     }
 };
 
+template <typename V>
+__device__ __forceinline__ V wave_max(V x) {
+#pragma unroll
+    for (int off = 32; off; off >>= 1) {
+        const V o = __shfl_xor(x, off);
+        x = o > x ? o : x;
+    }
+    return x;
+}
 template <typename V>
 __device__ __forceinline__ V wave_sum(V x) {
 #pragma unroll
@@ -98,102 +209,415 @@ __device__ __forceinline__ Found<V> find_prefix(const V* part, int n, int lane, 
     return f;
 }
 
+// One wavefront per block of 2048 logits, four blocks per workgroup.
 template <bool BF16>
-__global__ void __launch_bounds__(kSampleThreads) k_sample(const SampleArgs a) {
-    constexpr int ES = BF16 ? 2 : 4;
-    __shared__ float s_f[kSampleWaves];
-    __shared__ int s_i[kSampleWaves];
-    __shared__ unsigned long long s_hist[256];
-    __shared__ double s_sum[kSampleMaxIters * kSampleWaves];
-    __shared__ uint32_t s_cnt[kSampleMaxIters * kSampleWaves];
+__global__ void __launch_bounds__(kThreads) k_sample_blocks(const SampleArgs a) {
+    const int lane = threadIdx.x & 63;
+    const int row = blockIdx.x / a.wg_per_row;
+    const int blk = (blockIdx.x - row * a.wg_per_row) * (kThreads / 64) + __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    const int b = row / a.T, i = row - b * a.T;
+    if (blk >= a.n_blocks || (a.n_query && i >= a.n_query[b])) return;
+    const SampleRow<BF16> logits(a, b, i);
+    float x[4][8];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) logits.load(blk * kSampleChunks + k * 64 + lane, x[k]);
+    const SampleRule rule = sample_rule(a, b);
+    float m[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        m[k] = x[k][0];
+#pragma unroll
+        for (int j = 1; j < 8; ++j) m[k] = fmaxf(m[k], x[k][j]);
+    }
+    const float M = wave_max(fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])));
+    if (rule.filters()) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            a.maxima[(int64_t)row * a.n_blocks * kSampleChunks + blk * kSampleChunks + k * 64 + lane] = (uint16_t)(order_key(m[k]) >> 16);
+    }
+    double sum = 0.0;
+    if (rule.sums() && M != -INFINITY) {
+        const double Md = (double)M;
+        double part[4] = {0.0, 0.0, 0.0, 0.0};
+        if (M == INFINITY) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) part[k] += x[k][j] == M ? 1.0 : 0.0;
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) part[k] += exp2_64(((double)x[k][j] - Md) * rule.c);
+        }
+        sum = wave_sum((part[0] + part[1]) + (part[2] + part[3]));
+    }
+    if (lane == 0) a.blocks[(int64_t)row * a.n_blocks + blk] = SampleBlock{sum, (double)M};
+}
+
+// ---- within one workgroup of kSampleThreads
+// Exclusive prefix sums over the threads, and the total.
+template <typename V>
+__device__ __forceinline__ V block_scan(V x, V* s_part, int tid, V& total) {
+    const int lane = tid & 63, wave = tid >> 6;
+    const V incl = wave_incl_scan(x, lane);
+    if (lane == 63) s_part[wave] = incl;
+    __syncthreads();
+    V before = 0;
+    total = 0;
+#pragma unroll
+    for (int w = 0; w < kSampleWaves; ++w) {
+        if (w == wave) before = total;
+        total += s_part[w];
+    }
+    __syncthreads();
+    return before + incl - x;
+}
+template <typename V>
+__device__ __forceinline__ V block_max(V x, V* s_part, int tid) {
+    x = wave_max(x);
+    if ((tid & 63) == 0) s_part[tid >> 6] = x;
+    __syncthreads();
+    x = s_part[0];
+#pragma unroll
+    for (int w = 1; w < kSampleWaves; ++w) x = s_part[w] > x ? s_part[w] : x;
+    __syncthreads();
+    return x;
+}
+
+// A list entry: larger is earlier in the order (logit descending, index ascending).
+__device__ __forceinline__ uint64_t list_entry(uint32_t key, int e) { return (uint64_t)key << 32 | (0xffffffffu - (uint32_t)e); }
+__device__ __forceinline__ float entry_value(uint64_t x) { return key_value((uint32_t)(x >> 32)); }
+__device__ __forceinline__ int entry_index(uint64_t x) { return (int)(0xffffffffu - (uint32_t)x); }
+
+// Token and probability from the weights w of the E entries of each thread, threads and entries in index order; e: their indices.
+template <int E>
+__device__ __forceinline__ void pick_in_order(const double (&w)[E], const int (&e)[E], float u, double* s_part, int* s_int, int tid, int32_t* token, float* prob) {
+    double sum = 0.0, total;
+#pragma unroll
+    for (int j = 0; j < E; ++j) sum += w[j];
+    const double before = block_scan(sum, s_part, tid, total);
+    const double target = (double)u * total;
+    // the first thread that passes the target, or else the last one with a weight
+    const bool over = sum > 0.0 && before + sum > target && u < 1.f;
+    const int who = block_max(over ? 0x40000000 - tid : (sum > 0.0 ? tid - 0x40000000 : -0x7fffffff), s_int, tid);
+    if (who != (over ? 0x40000000 - tid : (sum > 0.0 ? tid - 0x40000000 : 0x7fffffff))) return;
+    double run = before, wf = 0.0;
+    int at = 0;
+    bool found = false;
+#pragma unroll
+    for (int j = 0; j < E; ++j) {
+        run += w[j];
+        if (w[j] > 0.0 && !found) {
+            at = e[j];
+            wf = w[j];
+            found = over && run > target;
+        }
+    }
+    *token = at;
+    if (prob) *prob = (float)(wf / total);
+}
+
+template <bool BF16>
+__global__ void __launch_bounds__(kSampleThreads) k_sample_pick(const SampleArgs a) {
+    __shared__ __align__(16) char s_mem[kSampleList * 20];
+    __shared__ double s_part[kSampleWaves];
+    __shared__ float s_float[kSampleWaves];
+    __shared__ int s_int[kSampleWaves], s_count[16];
     __shared__ uint32_t s_digit;
     __shared__ unsigned long long s_above;
+    static_assert(kSampleMaxIters * kSampleWaves * 12 + 256 * 8 <= sizeof(s_mem) && kSampleMaxBlocks * 8 <= sizeof(s_mem), "one array for every way");
 
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int row = blockIdx.x, b = row / a.T, i = row - b * a.T;
+    int32_t* const token = a.tokens + row;
+    float* const prob = a.probs ? a.probs + row : nullptr;
     if (a.n_query && i >= a.n_query[b]) {
         if (tid == 0) {
-            a.tokens[row] = -1;
-            if (a.probs) a.probs[row] = 0.f;
+            *token = -1;
+            if (prob) *prob = 0.f;
         }
         return;
     }
-    const char* base = a.logits + b * a.s[0] + i * a.s[1];
-    const int shift = (int)((uintptr_t)base & 15) / ES;        // elements of the first chunk that lie before the row
-    const int n_chunks = (a.V + shift + 7) / 8, iters = (n_chunks + kSampleThreads - 1) / kSampleThreads;
+    const SampleBlock* blocks = a.blocks + (int64_t)row * a.n_blocks;
+    const SampleRow<BF16> logits(a, b, i);
+    const SampleRule rule = sample_rule(a, b);
+    float u = a.u[row];
+    u = u >= 0.f ? fminf(u, 1.f) : 0.f;
 
-    // chunk c: elements 8 c - shift .. + 7; elements outside the row read as -inf, NaN counts as -inf, -0 as 0
-    auto load8 = [&](int c, float (&x)[8]) {
-        const int e0 = 8 * c - shift;
-        if (e0 >= 0 && e0 + 8 <= a.V) {
-            const u32x4* p = reinterpret_cast<const u32x4*>(base + (int64_t)e0 * ES);
-            if constexpr (BF16) {
-                const u32x4 v = *p;
+    float mx = -INFINITY;
+    for (int k = tid; k < a.n_blocks; k += kSampleThreads) mx = fmaxf(mx, (float)blocks[k].max);
+    mx = block_max(mx, s_float, tid);
+    if (mx == -INFINITY) {
+        if (tid == 0) {
+            *token = -1;
+            if (prob) *prob = 0.f;
+        }
+        return;
+    }
+    if (rule.first) {
+        int at = -0x7fffffff;      // minus the first block that holds the maximum
+        for (int k = tid; k < a.n_blocks; k += kSampleThreads)
+            if ((float)blocks[k].max == mx) at = max(at, -k);
+        at = -block_max(at, s_int, tid);
+        int e = -0x7fffffff;
+        if (tid < kSampleChunks) {
+            float x[8];
+            logits.load(at * kSampleChunks + tid, x);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    x[2 * j] = __uint_as_float(v[j] << 16);
-                    x[2 * j + 1] = __uint_as_float(v[j] & 0xffff0000u);
-                }
-            } else {
-                const u32x4 v = p[0], w = p[1];
+            for (int j = 7; j >= 0; --j)
+                if (x[j] == mx) e = -(logits.first(at * kSampleChunks + tid) + j);
+        }
+        e = -block_max(e, s_int, tid);
+        if (tid == 0) {
+            *token = e;
+            if (prob) *prob = 1.f;
+        }
+        return;
+    }
+    const SampleWeight weight{(double)mx, rule.c, mx};
+
+    // ---- sums of the blocks against the row's maximum
+    double* s_sum = reinterpret_cast<double*>(s_mem);
+    double total = 0.0;
+    if (rule.sums()) {
+        double sum = 0.0;
+        for (int k = tid; k < a.n_blocks; k += kSampleThreads) {
+            const SampleBlock x = blocks[k];
+            const double v = x.sum == 0.0 ? 0.0 : x.sum * weight((float)x.max);
+            s_sum[k] = v;
+            sum += v;
+        }
+        block_scan(sum, s_part, tid, total);
+    }
+    if (!rule.filters()) {
+        if (wave) return;
+        const Found<double> f = find_prefix(s_sum, a.n_blocks, lane, [&](double all) { return (double)u * all; });
+        const double target = (double)u * f.total;
+        const bool past = u >= 1.f || f.before >= f.total;      // nothing exceeds the target: the last positive weight
+        double w[32], sum = 0.0;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    x[j] = __uint_as_float(v[j]);
-                    x[4 + j] = __uint_as_float(w[j]);
-                }
-            }
-        } else {
+        for (int k = 0; k < 4; ++k) {
+            float x[8];
+            logits.load(f.at * kSampleChunks + lane * 4 + k, x);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                x[j] = -INFINITY;
-                if (c < n_chunks && e0 + j >= 0 && e0 + j < a.V) {
-                    if constexpr (BF16) x[j] = __uint_as_float((uint32_t)reinterpret_cast<const uint16_t*>(base)[e0 + j] << 16);
-                    else x[j] = reinterpret_cast<const float*>(base)[e0 + j];
-                }
+                w[8 * k + j] = weight(x[j]);
+                sum += w[8 * k + j];
             }
         }
+        const int e0 = logits.first(f.at * kSampleChunks + lane * 4);
+        double run = f.before + wave_incl_scan(sum, lane) - sum, wf = 0.0;
+        int found = -1, last = -1;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = x[j] != x[j] ? -INFINITY : x[j] + 0.f;
-    };
+        for (int j = 0; j < 32; ++j) {
+            run += w[j];
+            if (w[j] > 0.0) {
+                if (found < 0) wf = w[j];
+                last = e0 + j;
+                if (found < 0 && run > target) found = last;
+            }
+        }
+        const uint64_t hit = past ? 0ull : __builtin_amdgcn_ballot_w64(found >= 0);
+        const uint64_t some = __builtin_amdgcn_ballot_w64(last >= 0);
+        const int who = hit ? (int)__builtin_ctzll(hit) : 63 - (int)__builtin_clzll(some | 1ull);
+        if (lane == who) {
+            if (!hit) {
+#pragma unroll
+                for (int j = 0; j < 32; ++j)
+                    if (w[j] > 0.0) wf = w[j];
+            }
+            *token = hit ? found : last;
+            if (prob) *prob = (float)(wf / f.total);
+        }
+        return;
+    }
+
+    // ---- a bound that no kept entry lies below, in upper halves of keys
+    const uint16_t* maxima = a.maxima + (int64_t)row * a.n_blocks * kSampleChunks;
+    const int n_max = a.n_blocks * kSampleChunks;
+    const int per = (n_max + 8 * kSampleThreads - 1) / (8 * kSampleThreads);      // groups of eight chunks per thread
+    uint32_t tau_m = 0;                      // min-p's threshold
+    if (rule.by_m) {
+        if (rule.min_p >= 1.f) {
+            tau_m = order_key(mx);
+        } else {
+            // the lowest key of weight min_p or more: within a few units of the key of M + t ln(min_p)
+            const uint32_t k0 = order_key((float)((double)mx + log((double)rule.min_p) * (double)rule.t));
+            const uint64_t reach = __builtin_amdgcn_ballot_w64(weight(key_value(k0 + (uint32_t)lane - 32u)) >= (double)rule.min_p);
+            tau_m = reach ? k0 + (uint32_t)__builtin_ctzll(reach) - 32u : order_key(mx);
+        }
+    }
+    uint32_t bound = 0;
+    bool listed = true;
+    if (rule.by_k) {
+        // the k-th largest of the maxima of groups of chunks: at least k logits are as large.  Four groups per thread.
+        listed = rule.top_k <= kSampleList / 2;
+        if (listed) {
+            uint32_t v[4] = {0, 0, 0, 0};
+            for (int g = 0; g < per; ++g) {
+                const int c = (tid * per + g) * 8;
+                if (c >= n_max) break;
+                const u32x4 x = *reinterpret_cast<const u32x4*>(maxima + c);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[j] = max(v[j], max(x[j] & 0xffffu, x[j] >> 16));
+            }
+            if (tid < 16) s_count[tid] = 0;
+            __syncthreads();
+            for (int bit = 15; bit >= 0; --bit) {
+                const uint32_t at = bound | 1u << bit;
+                int n = 0;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) n += __builtin_popcountll(__builtin_amdgcn_ballot_w64(v[j] >= at));
+                if (lane == 0) atomicAdd(&s_count[bit], n);
+                __syncthreads();
+                if (s_count[bit] >= rule.top_k) bound = at;
+            }
+        }
+    } else if (rule.by_p) {
+        // entries of weight below (1 - p) Z / V hold less than (1 - p) Z together
+        const double least = (1.0 - (double)rule.top_p) * (1.0 - 1e-9) * total / (double)a.V;
+        const uint32_t k = order_key(mx == INFINITY ? mx : (float)((double)mx + log(least) * (double)rule.t));
+        bound = (k > 2 ? k - 2 : 0) >> 16;
+    }
+    if (rule.by_m && !rule.by_p) bound = max(bound, tau_m >> 16);
+    bound = max(bound, order_key(-3.4028235e38f) >> 16);      // (entries of -inf are never kept)
+    const uint32_t bound_key = bound << 16;
+
+    // ---- the candidates, in index order
+    uint64_t* s_list = reinterpret_cast<uint64_t*>(s_mem);
+    uint32_t* s_chunk = reinterpret_cast<uint32_t*>(s_mem + kSampleList * 16);
+    int n_list = 0;
+    if (listed) {
+        uint32_t mine = 0;
+        for (int g = 0; g < per; ++g) {
+            const int c = (tid * per + g) * 8;
+            if (c >= n_max) break;
+            const u32x4 x = *reinterpret_cast<const u32x4*>(maxima + c);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) mine += ((x[j] & 0xffffu) >= bound ? 1 : 0) + ((x[j] >> 16) >= bound ? 1 : 0);
+        }
+        int n_hit;
+        int at = block_scan((int)mine, s_int, tid, n_hit);
+        listed = n_hit <= kSampleList;
+        if (listed) {
+            if (mine) {
+                for (int g = 0; g < per; ++g) {
+                    const int c = (tid * per + g) * 8;
+                    if (c >= n_max) break;
+                    const u32x4 x = *reinterpret_cast<const u32x4*>(maxima + c);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        if ((x[j] & 0xffffu) >= bound) s_chunk[at++] = c + 2 * j;
+                        if ((x[j] >> 16) >= bound) s_chunk[at++] = c + 2 * j + 1;
+                    }
+                }
+            }
+            __syncthreads();
+            float x[2][8];
+            int found = 0;
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                if (2 * tid + k >= n_hit) continue;
+                logits.load((int)s_chunk[2 * tid + k], x[k]);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) found += order_key(x[k][j]) >= bound_key ? 1 : 0;
+            }
+            int to = block_scan(found, s_int, tid, n_list);
+            listed = n_list <= kSampleList;
+            if (listed) {
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    if (2 * tid + k >= n_hit) continue;
+                    const int e0 = logits.first((int)s_chunk[2 * tid + k]);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        if (order_key(x[k][j]) >= bound_key) s_list[to++] = list_entry(order_key(x[k][j]), e0 + j);
+                }
+                __syncthreads();
+            }
+        }
+    }
+    if (listed) {
+        // ---- in order: bitonic sort of the smallest power of two that holds the list
+        uint64_t* s_sorted = s_list + kSampleList;
+        int size = 64;
+        while (size < n_list) size *= 2;
+        for (int k = tid; k < size; k += kSampleThreads) s_sorted[k] = k < n_list ? s_list[k] : 0ull;
+        __syncthreads();
+        for (int run = 2; run <= size; run *= 2)
+            for (int gap = run / 2; gap; gap /= 2) {
+                if (tid < size / 2) {
+                    const int lo = (tid & ~(gap - 1)) * 2 + (tid & (gap - 1)), hi = lo + gap;
+                    const uint64_t x = s_sorted[lo], y = s_sorted[hi];
+                    const bool descending = !(lo & run);
+                    if ((x < y) == descending) {
+                        s_sorted[lo] = y;
+                        s_sorted[hi] = x;
+                    }
+                }
+                __syncthreads();
+            }
+        // ---- how many are kept: two entries per thread, by rank
+        double w[2], cum[2], all;
+        uint64_t x[2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            x[k] = 2 * tid + k < n_list ? s_sorted[2 * tid + k] : 0ull;
+            w[k] = 2 * tid + k < n_list ? weight(entry_value(x[k])) : 0.0;
+        }
+        cum[0] = block_scan(w[0] + w[1], s_part, tid, all) + w[0];
+        cum[1] = cum[0] + w[1];
+        int n = rule.by_k ? min(rule.top_k, n_list) : n_list;
+        if (rule.by_p) {
+            if (rule.by_k) {       // the sum over the first k
+                if (n - 1 == 2 * tid || n - 1 == 2 * tid + 1) s_part[0] = cum[(n - 1) & 1];
+                __syncthreads();
+                total = s_part[0];
+                __syncthreads();
+            }
+            const double target = (double)rule.top_p * total;
+            int below = 0, sum;
+#pragma unroll
+            for (int k = 0; k < 2; ++k) below += 2 * tid + k < n && cum[k] < target ? 1 : 0;
+            block_scan(below, s_int, tid, sum);
+            n = min(n, sum + 1);
+        }
+        if (rule.by_m) {
+            int reach = 0, sum;
+#pragma unroll
+            for (int k = 0; k < 2; ++k) reach += 2 * tid + k < n && (uint32_t)(x[k] >> 32) >= tau_m ? 1 : 0;
+            block_scan(reach, s_int, tid, sum);
+            n = min(n, sum);
+        }
+        // ---- the kept entries in index order
+        const uint64_t last = s_sorted[max(n, 1) - 1];
+        int e[2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            x[k] = 2 * tid + k < n_list ? s_list[2 * tid + k] : 0ull;
+            e[k] = entry_index(x[k]);
+            w[k] = x[k] >= last ? weight(entry_value(x[k])) : 0.0;
+        }
+        pick_in_order<2>(w, e, u, s_part, s_int, tid, token, prob);
+        return;
+    }
+
+    // ---- the general way: radix selections over the row, re-read for every digit.  tau of top-k is selected by counts, tau of top-p by
+    //      mass; masses are summed as 64-bit fixed point, so the sums do not depend on the order of the atomics.
+    __syncthreads();
+    double* s_sums = reinterpret_cast<double*>(s_mem);
+    uint32_t* s_cnt = reinterpret_cast<uint32_t*>(s_mem + kSampleMaxIters * kSampleWaves * 8);
+    unsigned long long* s_hist = reinterpret_cast<unsigned long long*>(s_mem + kSampleMaxIters * kSampleWaves * 12);
+    const int iters = (logits.n_chunks + kSampleThreads - 1) / kSampleThreads;
     auto each = [&](auto&& body) {       // body(iteration, first element of the chunk, its eight values)
         for (int it = 0; it < iters; ++it) {
             const int c = it * kSampleThreads + tid;
             float x[8];
-            load8(c, x);
-            body(it, 8 * c - shift, x);
+            logits.load(c, x);
+            body(it, logits.first(c), x);
         }
     };
-
-    // ---- the maximum
-    float mx = -INFINITY;
-    each([&](int, int, const float (&x)[8]) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) mx = fmaxf(mx, x[j]);
-    });
-#pragma unroll
-    for (int off = 32; off; off >>= 1) mx = fmaxf(mx, __shfl_xor(mx, off));
-    if (lane == 0) s_f[wave] = mx;
-    __syncthreads();
-    mx = s_f[0];
-#pragma unroll
-    for (int w = 1; w < kSampleWaves; ++w) mx = fmaxf(mx, s_f[w]);
-    if (mx == -INFINITY) {
-        if (tid == 0) {
-            a.tokens[row] = -1;
-            if (a.probs) a.probs[row] = 0.f;
-        }
-        return;
-    }
-    const float t = a.temperature ? a.temperature[b] : 1.f;
-    const bool greedy = !(t > 0.f);
-    const SampleWeight weight{(double)mx, greedy ? 1.0 : 1.0 / (double)t, mx};
-    int top_k = a.top_k ? a.top_k[b] : 0;
-    float top_p = a.top_p ? a.top_p[b] : 1.f;
-    const float min_p = a.min_p ? a.min_p[b] : 0.f;
-    if (greedy || top_p <= 0.f) top_k = 1;
-    if (top_k <= 0 || top_k > a.V) top_k = a.V;
-    const bool by_k = top_k < a.V, by_p = top_k > 1 && top_p > 0.f && top_p < 1.f;
-
     uint32_t tau = 0, quota = 0xffffffffu;
     // ---- radix selection, eight bits at a time: the digit in which the sum from the top reaches `target`
     auto pick_digit = [&](double target, unsigned long long above) {      // s_hist -> s_digit, s_above
@@ -227,7 +651,7 @@ __global__ void __launch_bounds__(kSampleThreads) k_sample(const SampleArgs a) {
         }
         __syncthreads();
     };
-    if (by_k) {
+    if (rule.by_k) {
         unsigned long long above = 0;
         uint32_t prefix = 0;
         for (int sh = 24; sh >= 0; sh -= 8) {
@@ -241,14 +665,14 @@ __global__ void __launch_bounds__(kSampleThreads) k_sample(const SampleArgs a) {
                     if (in) atomicAdd(&s_hist[(k >> sh) & 255], 1ull);
                 }
             });
-            pick_digit((double)top_k, above);
+            pick_digit((double)rule.top_k, above);
             prefix = (prefix << 8) | s_digit;
             above = s_above;
         }
         tau = prefix;
-        quota = (uint32_t)(top_k - (int)above);
+        quota = (uint32_t)(rule.top_k - (int)above);
     }
-    if (by_p) {
+    if (rule.by_p) {
         const uint32_t tau_k = tau, quota_k = quota;
         auto mass = [&](uint32_t k) { return (unsigned long long)(weight(key_value(k)) * a.mass_scale + 0.5); };
         unsigned long long above = 0;
@@ -261,17 +685,17 @@ __global__ void __launch_bounds__(kSampleThreads) k_sample(const SampleArgs a) {
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
                     const uint32_t k = order_key(x[j]);
-                    if (k < tau_k || (by_k && k == tau_k) || x[j] == -INFINITY || (sh != 24 && (k >> (sh + 8)) != prefix)) continue;
+                    if (k < tau_k || (rule.by_k && k == tau_k) || x[j] == -INFINITY || (sh != 24 && (k >> (sh + 8)) != prefix)) continue;
                     const unsigned long long m = mass(k);
                     if (m) atomicAdd(&s_hist[(k >> sh) & 255], m);
                 }
             });
-            if (by_k && tid == 0 && (sh == 24 || (tau_k >> (sh + 8)) == prefix)) atomicAdd(&s_hist[(tau_k >> sh) & 255], quota_k * mass(tau_k));
+            if (rule.by_k && tid == 0 && (sh == 24 || (tau_k >> (sh + 8)) == prefix)) atomicAdd(&s_hist[(tau_k >> sh) & 255], quota_k * mass(tau_k));
             if (sh == 24) {
                 __syncthreads();
                 unsigned long long h = 0;
                 for (int d = lane; d < 256; d += 64) h += s_hist[d];
-                target = (double)top_p * (double)wave_sum(h);
+                target = (double)rule.top_p * (double)wave_sum(h);
             }
             pick_digit(target, above);
             prefix = (prefix << 8) | s_digit;
@@ -279,22 +703,14 @@ __global__ void __launch_bounds__(kSampleThreads) k_sample(const SampleArgs a) {
             __syncthreads();
         }
         const unsigned long long each_m = mass(prefix);
-        const uint32_t ties = (by_k && prefix == tau_k) ? quota_k : 0xffffffffu;
+        const uint32_t ties = (rule.by_k && prefix == tau_k) ? quota_k : 0xffffffffu;
         double m = ceil((target - (double)above) / (double)each_m);
         m = fmin(fmax(m, 1.0), (double)ties);
         tau = prefix;
         quota = (uint32_t)m;
     }
-    if (min_p >= 1.f) {
-        if (tau != order_key(mx)) quota = 0xffffffffu;
-        tau = order_key(mx);
-    } else if (min_p > 0.f && !(weight(key_value(tau)) >= (double)min_p)) {     // (tau = 0, no threshold yet, reads as NaN)
-        // the lowest key of weight min_p or more: within a few units of the key of M + t ln(min_p)
-        const float near = (float)((double)mx + log((double)min_p) * (double)t);
-        const uint32_t k0 = order_key(near);
-        const uint32_t k = k0 + (uint32_t)lane - 32u;
-        const uint64_t reach = __builtin_amdgcn_ballot_w64(weight(key_value(k)) >= (double)min_p);
-        tau = reach ? k0 + (uint32_t)__builtin_ctzll(reach) - 32u : order_key(mx);
+    if (rule.by_m && tau < tau_m) {
+        tau = tau_m;
         quota = 0xffffffffu;
     }
 
@@ -314,7 +730,7 @@ __global__ void __launch_bounds__(kSampleThreads) k_sample(const SampleArgs a) {
         if (f.total > quota) {
             float x[8];
             const int c = f.at * 64 + lane;
-            load8(c, x);
+            logits.load(c, x);
             uint32_t mine = 0;
 #pragma unroll
             for (int j = 0; j < 8; ++j) mine += order_key(x[j]) == tau ? 1u : 0u;
@@ -322,7 +738,7 @@ __global__ void __launch_bounds__(kSampleThreads) k_sample(const SampleArgs a) {
             int found = -1;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                if (order_key(x[j]) == tau && ++run == quota) found = 8 * c - shift + j;
+                if (order_key(x[j]) == tau && ++run == quota) found = 8 * c - logits.shift + j;
             }
             const uint64_t who = __builtin_amdgcn_ballot_w64(found >= 0);
             cut = __shfl(found, (int)__builtin_ctzll(who));
@@ -333,7 +749,7 @@ __global__ void __launch_bounds__(kSampleThreads) k_sample(const SampleArgs a) {
         return k > tau || (k == tau && e <= cut);
     };
 
-    // ---- sums of the kept weights by blocks of 512 consecutive elements, then the block, lane and element of u
+    // ---- sums of the kept weights by blocks of 512 consecutive elements, then the block and the element of u
     each([&](int it, int e0, const float (&x)[8]) {
         double sum = 0.0;
         bool any = false;
@@ -345,32 +761,30 @@ __global__ void __launch_bounds__(kSampleThreads) k_sample(const SampleArgs a) {
                 if (kept(x[j], e0 + j)) sum += weight(x[j]);
             sum = wave_sum(sum);
         }
-        if (lane == 0) s_sum[it * kSampleWaves + wave] = sum;
+        if (lane == 0) s_sums[it * kSampleWaves + wave] = sum;
     });
     __syncthreads();
-    if (wave != 0) return;
-    float u = a.u[row];
-    u = u >= 0.f ? fminf(u, 1.f) : 0.f;
-    const Found<double> f = find_prefix(s_sum, n_parts, lane, [&](double total) { return (double)u * total; });
+    const Found<double> f = find_prefix(s_sums, n_parts, lane, [&](double sum) { return (double)u * sum; });
+    if (wave) return;
     const double target = (double)u * f.total;
     const int c = f.at * 64 + lane;
     float x[8];
-    load8(c, x);
+    logits.load(c, x);
     double w[8], sum = 0.0;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-        w[j] = kept(x[j], 8 * c - shift + j) ? weight(x[j]) : 0.0;
+        w[j] = kept(x[j], 8 * c - logits.shift + j) ? weight(x[j]) : 0.0;
         sum += w[j];
     }
     double run = f.before + wave_incl_scan(sum, lane) - sum;
-    const bool past = f.before >= f.total;          // nothing exceeds the target: the last positive weight
+    const bool past = u >= 1.f || f.before >= f.total;          // nothing exceeds the target: the last positive weight
     int found = -1, last = -1;
     double wf = 0.0, wl = 0.0;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
         run += w[j];
         if (w[j] > 0.0) {
-            last = 8 * c - shift + j;
+            last = 8 * c - logits.shift + j;
             wl = w[j];
             if (found < 0 && run > target) {
                 found = last;
@@ -380,10 +794,10 @@ __global__ void __launch_bounds__(kSampleThreads) k_sample(const SampleArgs a) {
     }
     const uint64_t hit = past ? 0ull : __builtin_amdgcn_ballot_w64(found >= 0);
     const uint64_t pos = __builtin_amdgcn_ballot_w64(last >= 0);
-    const int who = hit ? (int)__builtin_ctzll(hit) : 63 - (int)__builtin_clzll(pos);
+    const int who = hit ? (int)__builtin_ctzll(hit) : 63 - (int)__builtin_clzll(pos | 1ull);
     if (lane == who) {
-        a.tokens[row] = hit ? found : last;
-        if (a.probs) a.probs[row] = (float)((hit ? wf : wl) / f.total);
+        *token = hit ? found : last;
+        if (prob) *prob = (float)((hit ? wf : wl) / f.total);
     }
 }
 

@@ -246,13 +246,18 @@ int sample_check(const ssv_sample_params* p, int64_t s[2]) {
     if (!p || p->B < 1 || p->T < 1 || p->V < 1) return SSV_EINVAL;
     if (p->dtype != SSV_F32 && p->dtype != SSV_BF16) return SSV_EINVAL;
     if (p->logits_stride[0] < 0 || p->logits_stride[1] < 0) return SSV_EINVAL;
-    if (p->V > SSV_SAMPLE_MAX_V || (int64_t)p->B * p->T >= (1ll << 31)) return SSV_EUNSUPPORTED;
+    if (p->V > SSV_SAMPLE_MAX_V || (int64_t)p->B * p->T * sample_blocks(p->V) >= (1ll << 28)) return SSV_EUNSUPPORTED;
     const int es = p->dtype == SSV_BF16 ? 2 : 4;
     const bool dense = !p->logits_stride[0] && !p->logits_stride[1];
     s[0] = (dense ? (int64_t)p->T * p->V : p->logits_stride[0]) * es;
     s[1] = (dense ? (int64_t)p->V : p->logits_stride[1]) * es;
     return SSV_OK;
 }
+
+size_t sample_blocks_bytes(const ssv_sample_params* p) {
+    return align_up((size_t)p->B * p->T * sample_blocks(p->V) * sizeof(SampleBlock), 256);
+}
+size_t sample_maxima_bytes(const ssv_sample_params* p) { return (size_t)p->B * p->T * sample_blocks(p->V) * kSampleChunks * 2; }
 
 }  // namespace
 
@@ -290,11 +295,14 @@ int ssv_prefix_verify(const void* q, const void* k_prefix, const void* v_prefix,
     return SSV_EUNSUPPORTED;
 }
 
-size_t ssv_sample_workspace_bytes(const ssv_sample_params*) { return 0; }
+size_t ssv_sample_workspace_bytes(const ssv_sample_params* p) {
+    int64_t s[2];
+    return sample_check(p, s) == SSV_OK ? sample_blocks_bytes(p) + sample_maxima_bytes(p) : 0;
+}
 
 int ssv_sample(const void* logits, const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p,
-               const float* u, const int32_t* n_query, const ssv_sample_params* p, int32_t* tokens, float* probs, void*, size_t,
-               void* stream) {
+               const float* u, const int32_t* n_query, const ssv_sample_params* p, int32_t* tokens, float* probs,
+               void* workspace, size_t workspace_bytes, void* stream) {
     SampleArgs a{};
     const int rc = sample_check(p, a.s);
     if (rc != SSV_OK) return rc;
@@ -303,16 +311,28 @@ int ssv_sample(const void* logits, const float* temperature, const int32_t* top_
     const void* words[] = {temperature, top_k, top_p, min_p, u, n_query, tokens, probs};
     for (const void* w : words)
         if (misaligned(w, 4)) return SSV_EINVAL;
+    if (!workspace || misaligned(workspace, 256) || workspace_bytes < sample_blocks_bytes(p) + sample_maxima_bytes(p)) return SSV_EWORKSPACE;
     a.logits = (const char*)logits;
     a.temperature = temperature; a.top_p = top_p; a.min_p = min_p; a.u = u; a.top_k = top_k; a.n_query = n_query;
     a.tokens = tokens; a.probs = probs;
+    a.blocks = (SampleBlock*)workspace;
+    a.maxima = (uint16_t*)((char*)workspace + sample_blocks_bytes(p));
     a.T = p->T; a.V = p->V;
+    a.n_blocks = sample_blocks(p->V);
+    a.wg_per_row = ceil_div(a.n_blocks, kThreads / 64);
     int bits = 0;
     while ((1 << bits) < p->V) ++bits;
     a.mass_scale = std::ldexp(1.0, 62 - bits);
-    const dim3 grid(p->B * p->T);
-    if (p->dtype == SSV_BF16) hipLaunchKernelGGL(k_sample<true>, grid, dim3(kSampleThreads), 0, (hipStream_t)stream, a);
-    else hipLaunchKernelGGL(k_sample<false>, grid, dim3(kSampleThreads), 0, (hipStream_t)stream, a);
+    const dim3 grid(p->B * p->T * a.wg_per_row), rows(p->B * p->T);
+    if (p->dtype == SSV_BF16) {
+        hipLaunchKernelGGL(k_sample_blocks<true>, grid, dim3(kThreads), 0, (hipStream_t)stream, a);
+        if (hipGetLastError() != hipSuccess) return SSV_ELAUNCH;
+        hipLaunchKernelGGL(k_sample_pick<true>, rows, dim3(kSampleThreads), 0, (hipStream_t)stream, a);
+    } else {
+        hipLaunchKernelGGL(k_sample_blocks<false>, grid, dim3(kThreads), 0, (hipStream_t)stream, a);
+        if (hipGetLastError() != hipSuccess) return SSV_ELAUNCH;
+        hipLaunchKernelGGL(k_sample_pick<false>, rows, dim3(kSampleThreads), 0, (hipStream_t)stream, a);
+    }
     return hipGetLastError() == hipSuccess ? SSV_OK : SSV_ELAUNCH;
 }
 

@@ -110,6 +110,18 @@ def test_sample_refuses_pointers():
             assert e.value.code == B.SSV_EINVAL
 
 
+def test_sample_refuses_workspaces():
+    for V in (1, 2041, 2042, 100003, B.SSV_SAMPLE_MAX_V):
+        p = B.make_sample_params(B=2, T=3, V=V, dtype=B.SSV_F32)
+        need = B.ssv_sample_workspace_bytes(p)
+        assert need > 0
+        for ws, size in ((None, need), (P16 + 128, need), (P16, need - 1)):
+            with pytest.raises(B.SsvError) as e:
+                B.ssv_sample(P16, None, None, None, None, P16, None, p, P16, None, ws, size, 0)
+            assert e.value.code == B.SSV_EWORKSPACE
+    assert B.ssv_sample_workspace_bytes(B.make_sample_params(B=0, T=3, V=8, dtype=B.SSV_F32)) == 0
+
+
 def test_accept_refusals():
     def code(B_=2, T=3, at=None, to=None):
         args = [P16] * 6 + [B_, T] + [P16] * 4
