@@ -8,9 +8,9 @@
 // Two launches.  k_sample_blocks reads the logits once, 2048 per wavefront over the whole chip, and leaves per block of 2048 the
 // maximum and (where the whole vocabulary counts) the sum of weights against it, and per chunk of 8 the upper half of the
 // maximum's key.  k_sample_pick, one workgroup per row, finds the token from these: without filters by the block in which the
-// running sum passes u, of which alone the logits are read again; with filters from a list of candidates, the logits above a bound that no
-// kept entry can lie below, sorted in LDS.  Rows whose filters keep more than the list holds take the general way, radix
-// selections over the row.
+// running sum passes u, of which alone the logits are read again; with filters from a list of candidates in LDS, the logits above
+// a bound that no kept entry can lie below (from histograms of the chunks' maxima), and only the histogram bin in which the
+// threshold falls is sorted.  Rows whose filters keep more than the list holds take the general way, radix selections over the row.
 #pragma once
 #include "device_common.hpp"
 
@@ -32,12 +32,15 @@ struct SampleArgs {
     double mass_scale;     // fixed-point units of a weight of 1: V times it stays below 2^63
 };
 
-constexpr int kSampleThreads = 1024, kSampleWaves = kSampleThreads / 64;
+constexpr int kSampleThreads = 256, kSampleWaves = kSampleThreads / 64;     // of k_sample_pick
 constexpr int kSampleMaxV = 1 << 20;
 constexpr int kSampleBlock = 2048, kSampleChunks = kSampleBlock / 8;
 constexpr int kSampleMaxBlocks = kSampleMaxV / kSampleBlock + 1;            // (an unaligned row starts inside its first chunk)
 constexpr int kSampleMaxIters = kSampleMaxV / (8 * kSampleThreads) + 1;
-constexpr int kSampleList = 2048;                                           // candidates that k_sample_pick sorts
+constexpr int kSampleList = 4096;                                           // candidates that k_sample_pick holds ...
+constexpr int kSampleSort = 2048;                                           // ... and sorts, of one bin
+constexpr int kSampleBins = 256;
+static_assert(kSampleThreads == kSampleChunks && kSampleThreads >= kSampleBins, "one thread per chunk of a block, and per bin");
 
 __host__ __device__ __forceinline__ int sample_blocks(int V) { return (V + 7 + kSampleBlock - 1) / kSampleBlock; }
 
@@ -290,43 +293,20 @@ __device__ __forceinline__ uint64_t list_entry(uint32_t key, int e) { return (ui
 __device__ __forceinline__ float entry_value(uint64_t x) { return key_value((uint32_t)(x >> 32)); }
 __device__ __forceinline__ int entry_index(uint64_t x) { return (int)(0xffffffffu - (uint32_t)x); }
 
-// Token and probability from the weights w of the E entries of each thread, threads and entries in index order; e: their indices.
-template <int E>
-__device__ __forceinline__ void pick_in_order(const double (&w)[E], const int (&e)[E], float u, double* s_part, int* s_int, int tid, int32_t* token, float* prob) {
-    double sum = 0.0, total;
-#pragma unroll
-    for (int j = 0; j < E; ++j) sum += w[j];
-    const double before = block_scan(sum, s_part, tid, total);
-    const double target = (double)u * total;
-    // the first thread that passes the target, or else the last one with a weight
-    const bool over = sum > 0.0 && before + sum > target && u < 1.f;
-    const int who = block_max(over ? 0x40000000 - tid : (sum > 0.0 ? tid - 0x40000000 : -0x7fffffff), s_int, tid);
-    if (who != (over ? 0x40000000 - tid : (sum > 0.0 ? tid - 0x40000000 : 0x7fffffff))) return;
-    double run = before, wf = 0.0;
-    int at = 0;
-    bool found = false;
-#pragma unroll
-    for (int j = 0; j < E; ++j) {
-        run += w[j];
-        if (w[j] > 0.0 && !found) {
-            at = e[j];
-            wf = w[j];
-            found = over && run > target;
-        }
-    }
-    *token = at;
-    if (prob) *prob = (float)(wf / total);
-}
+struct BinFound { int bin, reached; uint32_t before; unsigned long long mass; };      // before, mass: of the bins ahead of it
 
 template <bool BF16>
 __global__ void __launch_bounds__(kSampleThreads) k_sample_pick(const SampleArgs a) {
-    __shared__ __align__(16) char s_mem[kSampleList * 20];
+    __shared__ __align__(16) char s_mem[kSampleList * 8];
+    __shared__ uint64_t s_sorted[kSampleSort];
+    __shared__ unsigned long long s_mass[kSampleBins], s_above, s_part64[kSampleWaves];
+    __shared__ uint32_t s_count[kSampleBins], s_digit;
     __shared__ double s_part[kSampleWaves];
     __shared__ float s_float[kSampleWaves];
-    __shared__ int s_int[kSampleWaves], s_count[16];
-    __shared__ uint32_t s_digit;
-    __shared__ unsigned long long s_above;
+    __shared__ int s_int[kSampleWaves];
+    __shared__ BinFound s_bin;
     static_assert(kSampleMaxIters * kSampleWaves * 12 + 256 * 8 <= sizeof(s_mem) && kSampleMaxBlocks * 8 <= sizeof(s_mem), "one array for every way");
+    static_assert(sizeof(s_sorted) == kSampleList * 4, "the chunks of the candidates lie where a bin is sorted later");
 
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int row = blockIdx.x, b = row / a.T, i = row - b * a.T;
@@ -361,13 +341,11 @@ __global__ void __launch_bounds__(kSampleThreads) k_sample_pick(const SampleArgs
             if ((float)blocks[k].max == mx) at = max(at, -k);
         at = -block_max(at, s_int, tid);
         int e = -0x7fffffff;
-        if (tid < kSampleChunks) {
-            float x[8];
-            logits.load(at * kSampleChunks + tid, x);
+        float x[8];
+        logits.load(at * kSampleChunks + tid, x);
 #pragma unroll
-            for (int j = 7; j >= 0; --j)
-                if (x[j] == mx) e = -(logits.first(at * kSampleChunks + tid) + j);
-        }
+        for (int j = 7; j >= 0; --j)
+            if (x[j] == mx) e = -(logits.first(at * kSampleChunks + tid) + j);
         e = -block_max(e, s_int, tid);
         if (tid == 0) {
             *token = e;
@@ -433,10 +411,21 @@ __global__ void __launch_bounds__(kSampleThreads) k_sample_pick(const SampleArgs
         return;
     }
 
-    // ---- a bound that no kept entry lies below, in upper halves of keys
+    // ---- lo: a value that no kept entry lies below
     const uint16_t* maxima = a.maxima + (int64_t)row * a.n_blocks * kSampleChunks;
-    const int n_max = a.n_blocks * kSampleChunks;
-    const int per = (n_max + 8 * kSampleThreads - 1) / (8 * kSampleThreads);      // groups of eight chunks per thread
+    const int n_groups8 = a.n_blocks * (kSampleChunks / 8);
+    auto each_max = [&](auto&& body) {       // body(iteration, chunk, upper half of its maximum's key); chunks in index order over (iteration, thread, call)
+        for (int it = 0; it * kSampleThreads < n_groups8; ++it) {
+            const int g = it * kSampleThreads + tid;
+            const u32x4 x = *reinterpret_cast<const u32x4*>(maxima + 8 * min(g, n_groups8 - 1));
+            if (g >= n_groups8) continue;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                body(it, 8 * g + 2 * j, x[j] & 0xffffu);
+                body(it, 8 * g + 2 * j + 1, x[j] >> 16);
+            }
+        }
+    };
     uint32_t tau_m = 0;                      // min-p's threshold
     if (rule.by_m) {
         if (rule.min_p >= 1.f) {
@@ -448,158 +437,304 @@ __global__ void __launch_bounds__(kSampleThreads) k_sample_pick(const SampleArgs
             tau_m = reach ? k0 + (uint32_t)__builtin_ctzll(reach) - 32u : order_key(mx);
         }
     }
-    uint32_t bound = 0;
-    bool listed = true;
+    const uint32_t lowest = order_key(-3.4028235e38f);      // (entries of -inf are never kept)
+    uint32_t lo = lowest;
     if (rule.by_k) {
-        // the k-th largest of the maxima of groups of chunks: at least k logits are as large.  Four groups per thread.
-        listed = rule.top_k <= kSampleList / 2;
-        if (listed) {
-            uint32_t v[4] = {0, 0, 0, 0};
-            for (int g = 0; g < per; ++g) {
-                const int c = (tid * per + g) * 8;
-                if (c >= n_max) break;
-                const u32x4 x = *reinterpret_cast<const u32x4*>(maxima + c);
+        // the least of the maxima of up to 1024 groups of chunks: as many logits are as large; or that of all chunks
+        uint32_t least = 0xffffu, of_groups = 0xffffu, v[4] = {0, 0, 0, 0};
+        int groups = 0, chunks = 0, n_groups, n_chunks;
+        each_max([&](int, int c, uint32_t x) {
+            const bool any = x >= lowest >> 16;
+            chunks += any ? 1 : 0;
+            least = any ? min(least, x) : least;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) v[j] = max(v[j], max(x[j] & 0xffffu, x[j] >> 16));
-            }
-            if (tid < 16) s_count[tid] = 0;
-            __syncthreads();
-            for (int bit = 15; bit >= 0; --bit) {
-                const uint32_t at = bound | 1u << bit;
-                int n = 0;
+            for (int j = 0; j < 4; ++j) v[j] = (c >> 1 & 3) == j ? max(v[j], x) : v[j];
+        });
 #pragma unroll
-                for (int j = 0; j < 4; ++j) n += __builtin_popcountll(__builtin_amdgcn_ballot_w64(v[j] >= at));
-                if (lane == 0) atomicAdd(&s_count[bit], n);
-                __syncthreads();
-                if (s_count[bit] >= rule.top_k) bound = at;
+        for (int j = 0; j < 4; ++j)
+            if (v[j] >= lowest >> 16) {
+                ++groups;
+                of_groups = min(of_groups, v[j]);
             }
-        }
+        block_scan(groups, s_int, tid, n_groups);
+        block_scan(chunks, s_int, tid, n_chunks);
+        if (n_groups >= rule.top_k) lo = (uint32_t)(0xffff - block_max((int)(0xffffu - of_groups), s_int, tid)) << 16;
+        else if (n_chunks >= rule.top_k) lo = (uint32_t)(0xffff - block_max((int)(0xffffu - least), s_int, tid)) << 16;
     } else if (rule.by_p) {
         // entries of weight below (1 - p) Z / V hold less than (1 - p) Z together
         const double least = (1.0 - (double)rule.top_p) * (1.0 - 1e-9) * total / (double)a.V;
         const uint32_t k = order_key(mx == INFINITY ? mx : (float)((double)mx + log(least) * (double)rule.t));
-        bound = (k > 2 ? k - 2 : 0) >> 16;
+        lo = max(lo, k > 2 ? k - 2 : 0);
     }
-    if (rule.by_m && !rule.by_p) bound = max(bound, tau_m >> 16);
-    bound = max(bound, order_key(-3.4028235e38f) >> 16);      // (entries of -inf are never kept)
-    const uint32_t bound_key = bound << 16;
+    if (rule.by_m && !rule.by_p) lo = max(lo, tau_m);
+    lo = max(lo, lowest);
 
-    // ---- the candidates, in index order
-    uint64_t* s_list = reinterpret_cast<uint64_t*>(s_mem);
-    uint32_t* s_chunk = reinterpret_cast<uint32_t*>(s_mem + kSampleList * 16);
-    int n_list = 0;
-    if (listed) {
-        uint32_t mine = 0;
-        for (int g = 0; g < per; ++g) {
-            const int c = (tid * per + g) * 8;
-            if (c >= n_max) break;
-            const u32x4 x = *reinterpret_cast<const u32x4*>(maxima + c);
+    // ---- bins of equal width from the maximum down to lo
+    const float width = mx - key_value(lo);
+    const float inv = width > 0.f && width < INFINITY ? (float)kSampleBins / width : 0.f;
+    auto bin_of = [&](float x) { return x == mx ? 0 : min(kSampleBins - 1, (int)((mx - x) * inv)); };
+    auto mass = [&](uint32_t k) { return (unsigned long long)(weight(key_value(k)) * a.mass_scale + 0.5); };
+    auto clear_bins = [&] {
+        s_mass[tid] = 0;
+        s_count[tid] = 0;
+        __syncthreads();
+    };
+    // The first bin up to which the entries number `n` or more, or weigh `m` or more (the last one that holds any, if none does).
+    auto find_bin = [&](bool by_mass, uint32_t n, double m) {
+        __syncthreads();
+        if (wave == 0) {
+            constexpr int PER = kSampleBins / 64;
+            uint32_t c[PER], cs = 0;
+            unsigned long long w[PER], ws = 0;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) mine += ((x[j] & 0xffffu) >= bound ? 1 : 0) + ((x[j] >> 16) >= bound ? 1 : 0);
+            for (int j = 0; j < PER; ++j) {
+                c[j] = s_count[PER * lane + j];
+                w[j] = s_mass[PER * lane + j];
+                cs += c[j];
+                ws += w[j];
+            }
+            const uint32_t ci = wave_incl_scan(cs, lane);
+            const unsigned long long wi = wave_incl_scan(ws, lane);
+            const uint64_t reached = __builtin_amdgcn_ballot_w64(cs > 0 && (by_mass ? (double)wi >= m : ci >= n));
+            const uint64_t some = __builtin_amdgcn_ballot_w64(cs > 0);
+            const int who = reached ? (int)__builtin_ctzll(reached) : 63 - (int)__builtin_clzll(some | 1ull);
+            if (lane == who) {
+                BinFound f{0, reached != 0, 0u, 0ull};
+                uint32_t run = ci - cs;
+                unsigned long long weigh = wi - ws;
+#pragma unroll
+                for (int j = 0; j < PER; ++j) {
+                    if (c[j] == 0 || (f.reached == 2)) continue;
+                    f.bin = PER * lane + j;
+                    f.before = run;
+                    f.mass = weigh;
+                    run += c[j];
+                    weigh += w[j];
+                    if (reached && (by_mass ? (double)weigh >= m : run >= n)) f.reached = 2;
+                }
+                s_bin = f;
+            }
         }
-        int n_hit;
-        int at = block_scan((int)mine, s_int, tid, n_hit);
-        listed = n_hit <= kSampleList;
-        if (listed) {
-            if (mine) {
-                for (int g = 0; g < per; ++g) {
-                    const int c = (tid * per + g) * 8;
-                    if (c >= n_max) break;
-                    const u32x4 x = *reinterpret_cast<const u32x4*>(maxima + c);
+        __syncthreads();
+        return s_bin;
+    };
+    // First over the chunks' maxima (their lower ends): where these alone suffice, nothing beyond that bin is kept.
+    int last_bin = kSampleBins - 1;
+    if (rule.by_k || rule.by_p) {
+        clear_bins();
+        each_max([&](int, int, uint32_t x) {
+            const uint32_t key = x << 16;
+            if (key < lo) return;
+            const int at = bin_of(key_value(key));
+            atomicAdd(&s_count[at], 1u);
+            if (!rule.by_k) atomicAdd(&s_mass[at], mass(key));
+        });
+        const BinFound f = find_bin(!rule.by_k, (uint32_t)rule.top_k, (double)rule.top_p * (1.0 + 1e-9) * total * a.mass_scale);
+        if (f.reached) last_bin = f.bin;
+    }
+
+    // ---- the candidates, in index order: chunks that may hold one (by the upper ends of their maxima), then the logits
+    uint64_t* s_list = reinterpret_cast<uint64_t*>(s_mem);
+    uint32_t* s_chunk = reinterpret_cast<uint32_t*>(s_sorted);
+    auto may_hold = [&](uint32_t half) {
+        const uint32_t key = half << 16 | 0xffffu;
+        return key >= lo && (key >= order_key(mx) || bin_of(key_value(key)) <= last_bin);
+    };
+    auto hits_of = [&](int it) {             // of this thread's eight chunks of an iteration
+        const int g = it * kSampleThreads + tid;
+        uint32_t hits = 0;
+        if (g < n_groups8) {
+            const u32x4 x = *reinterpret_cast<const u32x4*>(maxima + 8 * g);
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        if ((x[j] & 0xffffu) >= bound) s_chunk[at++] = c + 2 * j;
-                        if ((x[j] >> 16) >= bound) s_chunk[at++] = c + 2 * j + 1;
+            for (int j = 0; j < 4; ++j) hits |= (may_hold(x[j] & 0xffffu) ? 1u : 0u) << (2 * j) | (may_hold(x[j] >> 16) ? 2u : 0u) << (2 * j);
+        }
+        return hits;
+    };
+    auto count_before = [&](uint32_t hits, int& all) {      // hits of the wavefront's lanes before this one, and of all
+        const uint32_t c = (uint32_t)__builtin_popcount(hits);
+        int before = 0;
+        all = 0;
+#pragma unroll
+        for (int bit = 0; bit < 4; ++bit) {
+            const uint64_t m = __builtin_amdgcn_ballot_w64(c >> bit & 1u);
+            before += (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0u)) << bit;
+            all += __builtin_popcountll(m) << bit;
+        }
+        return before;
+    };
+    int n_hit = 0, n = 0;
+    {
+        // hits by (iteration, wavefront), their prefix sums, then the places
+        uint32_t* s_hits = reinterpret_cast<uint32_t*>(s_mem);
+        const int n_it = (n_groups8 + kSampleThreads - 1) / kSampleThreads;
+        for (int it = 0; it < n_it; ++it) {
+            int all;
+            count_before(hits_of(it), all);
+            if (lane == 0) s_hits[it * kSampleWaves + wave] = (uint32_t)all;
+        }
+        __syncthreads();
+        const int per = (n_it * kSampleWaves + kSampleThreads - 1) / kSampleThreads;
+        uint32_t sum = 0;
+        for (int k = tid * per; k < min(n_it * kSampleWaves, (tid + 1) * per); ++k) sum += s_hits[k];
+        int at = block_scan((int)sum, s_int, tid, n_hit);
+        for (int k = tid * per; k < min(n_it * kSampleWaves, (tid + 1) * per); ++k) {
+            const int c = (int)s_hits[k];
+            s_hits[k] = (uint32_t)at;
+            at += c;
+        }
+        __syncthreads();
+        if (n_hit <= kSampleList)
+            for (int it = 0; it < n_it; ++it) {
+                int all;
+                const uint32_t hits = hits_of(it);
+                int to = (int)s_hits[it * kSampleWaves + wave] + count_before(hits, all);
+                for (uint32_t rest = hits; rest; rest &= rest - 1) s_chunk[to++] = 8 * (it * kSampleThreads + tid) + __builtin_ctz(rest);
+            }
+        __syncthreads();
+    }
+    bool listed = n_hit <= kSampleList;
+    auto candidate = [&](float x) { return order_key(x) >= lo && bin_of(x) <= last_bin; };
+    if (listed) {
+        const int q = (n_hit + kSampleThreads - 1) / kSampleThreads, h0 = min(n_hit, tid * q), h1 = min(n_hit, h0 + q);
+        int mine = 0;
+        float x[8];
+        for (int h = h0; h < h1; ++h) {
+            logits.load((int)s_chunk[h], x);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) mine += candidate(x[j]) ? 1 : 0;
+        }
+        int at = block_scan(mine, s_int, tid, n);
+        listed = n <= kSampleList;
+        if (listed)
+            for (int h = h0; h < h1; ++h) {
+                if (q > 1) logits.load((int)s_chunk[h], x);
+                const int e0 = logits.first((int)s_chunk[h]);
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (candidate(x[j])) s_list[at++] = list_entry(order_key(x[j]), e0 + j);
+            }
+        __syncthreads();
+    }
+    const int q = (n + kSampleThreads - 1) / kSampleThreads, l0 = min(n, tid * q), l1 = min(n, l0 + q);     // this thread's entries
+    uint64_t last_kept = 0;             // the last entry that is kept
+    if (listed && (rule.by_k || rule.by_p)) {
+        // ---- the exact threshold: a histogram of the list, and the entries of the bin in which it falls in order
+        clear_bins();
+        for (int l = l0; l < l1; ++l) {
+            const uint32_t key = (uint32_t)(s_list[l] >> 32);
+            const int at = bin_of(key_value(key));
+            atomicAdd(&s_count[at], 1u);
+            if (rule.by_p) atomicAdd(&s_mass[at], mass(key));
+        }
+        // the entries of a bin into s_sorted, descending; how many
+        auto sort_bin = [&](int bin) {
+            int mine = 0, m;
+            for (int l = l0; l < l1; ++l) mine += bin_of(entry_value(s_list[l])) == bin ? 1 : 0;
+            int at = block_scan(mine, s_int, tid, m);
+            if (m > kSampleSort) return m;
+            for (int l = l0; l < l1; ++l)
+                if (bin_of(entry_value(s_list[l])) == bin) s_sorted[at++] = s_list[l];
+            int size = 64;
+            while (size < m) size *= 2;
+            for (int k = m + tid; k < size; k += kSampleThreads) s_sorted[k] = 0ull;
+            __syncthreads();
+            if (size == 64) {              // one wavefront, by lane exchanges
+                if (wave == 0) {
+                    uint64_t x = s_sorted[lane];
+#pragma unroll
+                    for (int run = 2; run <= 64; run *= 2)
+#pragma unroll
+                        for (int gap = run / 2; gap; gap /= 2) {
+                            const uint64_t y = __shfl_xor(x, gap);
+                            const bool larger = ((lane & gap) == 0) == ((lane & run) == 0);      // this lane keeps the larger one
+                            x = (x > y) == larger ? x : y;
+                        }
+                    s_sorted[lane] = x;
+                }
+                __syncthreads();
+                return m;
+            }
+            for (int run = 2; run <= size; run *= 2)
+                for (int gap = run / 2; gap; gap /= 2) {
+                    for (int k = tid; k < size / 2; k += kSampleThreads) {
+                        const int p = (k & ~(gap - 1)) * 2 + (k & (gap - 1));
+                        const uint64_t x = s_sorted[p], y = s_sorted[p + gap];
+                        if ((x < y) == !(p & run)) {
+                            s_sorted[p] = y;
+                            s_sorted[p + gap] = x;
+                        }
+                    }
+                    __syncthreads();
+                }
+            return m;
+        };
+        // of the first m sorted entries: how many come before the running mass from `base` reaches the target; their whole mass
+        auto reach_mass = [&](int m, unsigned long long base, double target, unsigned long long& all) {
+            const int s = (m + kSampleThreads - 1) / kSampleThreads, k0 = min(m, tid * s), k1 = min(m, k0 + s);
+            unsigned long long sum = 0;
+            for (int k = k0; k < k1; ++k) sum += mass((uint32_t)(s_sorted[k] >> 32));
+            unsigned long long run = base + block_scan(sum, s_part64, tid, all);
+            int below = 0, n_below;
+            for (int k = k0; k < k1; ++k) {
+                run += mass((uint32_t)(s_sorted[k] >> 32));
+                below += (double)run < target ? 1 : 0;
+            }
+            block_scan(below, s_int, tid, n_below);
+            return n_below;
+        };
+        double target = (double)rule.top_p * total * a.mass_scale;
+        bool done = false;
+        if (rule.by_k) {
+            const BinFound f = find_bin(false, (uint32_t)rule.top_k, 0.0);
+            const int m = sort_bin(f.bin);
+            listed = m <= kSampleSort;
+            if (listed) {
+                const int r = max(1, min(m, rule.top_k - (int)f.before));       // the k-th entry is the r-th of the bin (all, if there are fewer than k)
+                last_kept = s_sorted[r - 1];
+                if (rule.by_p) {
+                    unsigned long long all;
+                    reach_mass(r, 0ull, 0.0, all);
+                    target = (double)rule.top_p * (double)(f.mass + all);
+                    if ((double)f.mass < target) {
+                        last_kept = s_sorted[min(reach_mass(r, f.mass, target, all), r - 1)];
+                        done = true;
                     }
                 }
             }
-            __syncthreads();
-            float x[2][8];
-            int found = 0;
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                if (2 * tid + k >= n_hit) continue;
-                logits.load((int)s_chunk[2 * tid + k], x[k]);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) found += order_key(x[k][j]) >= bound_key ? 1 : 0;
-            }
-            int to = block_scan(found, s_int, tid, n_list);
-            listed = n_list <= kSampleList;
+        }
+        if (rule.by_p && listed && !done) {
+            const BinFound f = find_bin(true, 0u, target);
+            const int m = sort_bin(f.bin);
+            listed = m <= kSampleSort;
             if (listed) {
-#pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    if (2 * tid + k >= n_hit) continue;
-                    const int e0 = logits.first((int)s_chunk[2 * tid + k]);
-#pragma unroll
-                    for (int j = 0; j < 8; ++j)
-                        if (order_key(x[k][j]) >= bound_key) s_list[to++] = list_entry(order_key(x[k][j]), e0 + j);
-                }
-                __syncthreads();
+                unsigned long long all;
+                last_kept = s_sorted[max(0, min(reach_mass(m, f.mass, target, all), m - 1))];
             }
         }
     }
     if (listed) {
-        // ---- in order: bitonic sort of the smallest power of two that holds the list
-        uint64_t* s_sorted = s_list + kSampleList;
-        int size = 64;
-        while (size < n_list) size *= 2;
-        for (int k = tid; k < size; k += kSampleThreads) s_sorted[k] = k < n_list ? s_list[k] : 0ull;
-        __syncthreads();
-        for (int run = 2; run <= size; run *= 2)
-            for (int gap = run / 2; gap; gap /= 2) {
-                if (tid < size / 2) {
-                    const int lo = (tid & ~(gap - 1)) * 2 + (tid & (gap - 1)), hi = lo + gap;
-                    const uint64_t x = s_sorted[lo], y = s_sorted[hi];
-                    const bool descending = !(lo & run);
-                    if ((x < y) == descending) {
-                        s_sorted[lo] = y;
-                        s_sorted[hi] = x;
-                    }
-                }
-                __syncthreads();
-            }
-        // ---- how many are kept: two entries per thread, by rank
-        double w[2], cum[2], all;
-        uint64_t x[2];
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            x[k] = 2 * tid + k < n_list ? s_sorted[2 * tid + k] : 0ull;
-            w[k] = 2 * tid + k < n_list ? weight(entry_value(x[k])) : 0.0;
+        // ---- the kept entries in index order: the one whose running sum passes u
+        auto kept_weight = [&](uint64_t x) { return x >= last_kept && (uint32_t)(x >> 32) >= tau_m ? weight(entry_value(x)) : 0.0; };
+        double sum = 0.0, all;
+        for (int l = l0; l < l1; ++l) sum += kept_weight(s_list[l]);
+        const double before = block_scan(sum, s_part, tid, all);
+        const double target = (double)u * all;
+        // the first thread that passes the target, or else the last one with a weight
+        const bool over = sum > 0.0 && before + sum > target && u < 1.f;
+        const int claim = over ? 0x40000000 - tid : (sum > 0.0 ? tid - 0x40000000 : -0x7fffffff);
+        if (block_max(claim, s_int, tid) != claim || !(sum > 0.0)) return;
+        double run = before, wf = 0.0;
+        int at = 0;
+        for (int l = l0; l < l1; ++l) {
+            const double w = kept_weight(s_list[l]);
+            if (!(w > 0.0)) continue;
+            run += w;
+            at = entry_index(s_list[l]);
+            wf = w;
+            if (over && run > target) break;
         }
-        cum[0] = block_scan(w[0] + w[1], s_part, tid, all) + w[0];
-        cum[1] = cum[0] + w[1];
-        int n = rule.by_k ? min(rule.top_k, n_list) : n_list;
-        if (rule.by_p) {
-            if (rule.by_k) {       // the sum over the first k
-                if (n - 1 == 2 * tid || n - 1 == 2 * tid + 1) s_part[0] = cum[(n - 1) & 1];
-                __syncthreads();
-                total = s_part[0];
-                __syncthreads();
-            }
-            const double target = (double)rule.top_p * total;
-            int below = 0, sum;
-#pragma unroll
-            for (int k = 0; k < 2; ++k) below += 2 * tid + k < n && cum[k] < target ? 1 : 0;
-            block_scan(below, s_int, tid, sum);
-            n = min(n, sum + 1);
-        }
-        if (rule.by_m) {
-            int reach = 0, sum;
-#pragma unroll
-            for (int k = 0; k < 2; ++k) reach += 2 * tid + k < n && (uint32_t)(x[k] >> 32) >= tau_m ? 1 : 0;
-            block_scan(reach, s_int, tid, sum);
-            n = min(n, sum);
-        }
-        // ---- the kept entries in index order
-        const uint64_t last = s_sorted[max(n, 1) - 1];
-        int e[2];
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            x[k] = 2 * tid + k < n_list ? s_list[2 * tid + k] : 0ull;
-            e[k] = entry_index(x[k]);
-            w[k] = x[k] >= last ? weight(entry_value(x[k])) : 0.0;
-        }
-        pick_in_order<2>(w, e, u, s_part, s_int, tid, token, prob);
+        *token = at;
+        if (prob) *prob = (float)(wf / all);
         return;
     }
 
@@ -611,11 +746,13 @@ __global__ void __launch_bounds__(kSampleThreads) k_sample_pick(const SampleArgs
     unsigned long long* s_hist = reinterpret_cast<unsigned long long*>(s_mem + kSampleMaxIters * kSampleWaves * 12);
     const int iters = (logits.n_chunks + kSampleThreads - 1) / kSampleThreads;
     auto each = [&](auto&& body) {       // body(iteration, first element of the chunk, its eight values)
-        for (int it = 0; it < iters; ++it) {
-            const int c = it * kSampleThreads + tid;
-            float x[8];
-            logits.load(c, x);
-            body(it, logits.first(c), x);
+        for (int it = 0; it < iters; it += 4) {
+            float x[4][8];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) logits.load((it + k) * kSampleThreads + tid, x[k]);
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (it + k < iters) body(it + k, logits.first((it + k) * kSampleThreads + tid), x[k]);
         }
     };
     uint32_t tau = 0, quota = 0xffffffffu;
@@ -674,7 +811,6 @@ __global__ void __launch_bounds__(kSampleThreads) k_sample_pick(const SampleArgs
     }
     if (rule.by_p) {
         const uint32_t tau_k = tau, quota_k = quota;
-        auto mass = [&](uint32_t k) { return (unsigned long long)(weight(key_value(k)) * a.mass_scale + 0.5); };
         unsigned long long above = 0;
         uint32_t prefix = 0;
         double target = 0.0;
