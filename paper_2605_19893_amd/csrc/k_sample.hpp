@@ -28,11 +28,12 @@ struct SampleArgs {
     uint16_t* maxima;      // [row][n_blocks * 256]: upper half of the order key of each chunk's maximum
     int T, V, n_blocks;
     int wg_per_row;        // k_sample_blocks
+    FastDiv div_wg, div_T;
     int64_t s[2];          // bytes: sequence, node
     double mass_scale;     // fixed-point units of a weight of 1: V times it stays below 2^63
 };
 
-constexpr int kSampleThreads = 256, kSampleWaves = kSampleThreads / 64;     // of k_sample_pick
+constexpr int kSampleThreads = 512, kSampleWaves = kSampleThreads / 64;     // of k_sample_pick
 constexpr int kSampleMaxV = 1 << 20;
 constexpr int kSampleBlock = 2048, kSampleChunks = kSampleBlock / 8;
 constexpr int kSampleMaxBlocks = kSampleMaxV / kSampleBlock + 1;            // (an unaligned row starts inside its first chunk)
@@ -40,7 +41,7 @@ constexpr int kSampleMaxIters = kSampleMaxV / (8 * kSampleThreads) + 1;
 constexpr int kSampleList = 4096;                                           // candidates that k_sample_pick holds ...
 constexpr int kSampleSort = 2048;                                           // ... and sorts, of one bin
 constexpr int kSampleBins = 256;
-static_assert(kSampleThreads == kSampleChunks && kSampleThreads >= kSampleBins, "one thread per chunk of a block, and per bin");
+static_assert(kSampleThreads >= kSampleChunks && kSampleThreads >= kSampleBins, "a thread per chunk of a block, and per bin");
 
 __host__ __device__ __forceinline__ int sample_blocks(int V) { return (V + 7 + kSampleBlock - 1) / kSampleBlock; }
 
@@ -67,6 +68,27 @@ __device__ __forceinline__ double exp2_64(double y) {
     p = __builtin_fma(p, f, 0.69314718055995);
     p = __builtin_fma(p, f, 1.0);
     return __builtin_ldexp(p, (int)n);
+}
+
+// The same for y = d c, d <= 0 and d c >= -1000, without the slow conversions: adding 1.5 * 2^52 rounds to a whole number and leaves it in
+// the low bits, from where it goes into the exponent.
+__device__ __forceinline__ double exp2_64_normal(double d, double c) {
+    const double magic = 6755399441055744.0;
+    const double t = __builtin_fma(d, c, magic), f = __builtin_fma(d, c, magic - t);
+    double p = 7.072585949269223e-09;
+    p = __builtin_fma(p, f, 1.0208690299958306e-07);
+    p = __builtin_fma(p, f, 1.321544258792169e-06);
+    p = __builtin_fma(p, f, 1.5252657260200837e-05);
+    p = __builtin_fma(p, f, 0.0001540353044173605);
+    p = __builtin_fma(p, f, 0.0013333558230164974);
+    p = __builtin_fma(p, f, 0.009618129107606888);
+    p = __builtin_fma(p, f, 0.05550410866444772);
+    p = __builtin_fma(p, f, 0.24022650695910097);
+    p = __builtin_fma(p, f, 0.69314718055995);
+    p = __builtin_fma(p, f, 1.0);
+    const uint64_t bits = __builtin_bit_cast(uint64_t, p);
+    const uint32_t n = (uint32_t)__builtin_bit_cast(uint64_t, t);
+    return __builtin_bit_cast(double, (uint64_t)((uint32_t)(bits >> 32) + (n << 20)) << 32 | (uint32_t)bits);
 }
 
 // Weight of a logit against a maximum; 1 at the maximum, whatever that is.
@@ -101,75 +123,111 @@ __device__ __forceinline__ SampleRule sample_rule(const SampleArgs& a, int b) {
 }
 
 // A row of logits in chunks of 8 from a 16-byte boundary on: chunk c holds elements 8 c - shift .. + 7.  Elements outside the
-// row read as -inf, NaN counts as -inf, -0 as 0.
+// row read as -inf, NaN counts as -inf, -0 as 0.  A chunk comes in two steps, so that several fetches are in flight before the
+// first is looked at: every chunk that lies in the row as a whole is fetched without a condition, the first and the last one are
+// read by elements where they do not.
 template <bool BF16>
 struct SampleRow {
     static constexpr int ES = BF16 ? 2 : 4;
+    struct Raw { u32x4 v[BF16 ? 1 : 2]; };
     const char* base;
     int V, shift, n_chunks;
+    int lo, hi;            // chunks that lie in the row as a whole: [lo, hi)
     __device__ __forceinline__ SampleRow(const SampleArgs& a, int b, int i) : base(a.logits + b * a.s[0] + i * a.s[1]), V(a.V) {
         shift = (int)((uintptr_t)base & 15) / ES;
         n_chunks = (V + shift + 7) / 8;
+        lo = shift ? 1 : 0;
+        hi = (V + shift) / 8;
     }
     __device__ __forceinline__ int first(int c) const { return 8 * c - shift; }
     __device__ __forceinline__ static float clean(float x) { return fmaxf(x + 0.f, -INFINITY); }
-    __device__ __forceinline__ void load(int c, float (&x)[8]) const {
-        const int e0 = first(c);
-        if (e0 >= 0 && e0 + 8 <= V) {
-            const u32x4* p = reinterpret_cast<const u32x4*>(base + (int64_t)e0 * ES);
-            if constexpr (BF16) {
-                const u32x4 v = *p;
+    __device__ __forceinline__ Raw fetch(int c) const {
+        Raw r{};
+        if (lo < hi) {     // (uniform)
+            const u32x4* p = reinterpret_cast<const u32x4*>(base + (int64_t)first(min(max(c, lo), hi - 1)) * ES);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    x[2 * j] = __uint_as_float(v[j] << 16);
-                    x[2 * j + 1] = __uint_as_float(v[j] & 0xffff0000u);
-                }
-            } else {
-                const u32x4 v = p[0], w = p[1];
+            for (int k = 0; k < (BF16 ? 1 : 2); ++k) r.v[k] = p[k];
+        }
+        return r;
+    }
+    __device__ __forceinline__ void unpack(int c, const Raw& r, float (&x)[8]) const {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    x[j] = __uint_as_float(v[j]);
-                    x[4 + j] = __uint_as_float(w[j]);
-                }
-            }
-        } else {
+        for (int j = 0; j < 8; ++j) {
+            if constexpr (BF16) x[j] = __uint_as_float(j & 1 ? r.v[0][j >> 1] & 0xffff0000u : r.v[0][j >> 1] << 16);
+            else x[j] = __uint_as_float(r.v[j >> 2][j & 3]);
+        }
+        if (c < lo || c >= hi) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
+                const int e = first(c) + j;
                 x[j] = -INFINITY;
-                if (c < n_chunks && e0 + j >= 0 && e0 + j < V) {
-                    if constexpr (BF16) x[j] = __uint_as_float((uint32_t)reinterpret_cast<const uint16_t*>(base)[e0 + j] << 16);
-                    else x[j] = reinterpret_cast<const float*>(base)[e0 + j];
+                if (e >= 0 && e < V) {
+                    if constexpr (BF16) x[j] = __uint_as_float((uint32_t)reinterpret_cast<const uint16_t*>(base)[e] << 16);
+                    else x[j] = reinterpret_cast<const float*>(base)[e];
                 }
             }
         }
 #pragma unroll
         for (int j = 0; j < 8; ++j) x[j] = clean(x[j]);
     }
+    __device__ __forceinline__ void load(int c, float (&x)[8]) const { unpack(c, fetch(c), x); }
+    template <int N>
+    __device__ __forceinline__ void load_each(int c, int step, float (&x)[N][8]) const {      // chunks c, c + step, ...
+        Raw r[N];
+#pragma unroll
+        for (int k = 0; k < N; ++k) r[k] = fetch(c + k * step);
+#pragma unroll
+        for (int k = 0; k < N; ++k) unpack(c + k * step, r[k], x[k]);
+    }
 };
 
-template <typename V>
-__device__ __forceinline__ V wave_max(V x) {
+// Scans of a wavefront through the lane shifts of the vector pipe (a step takes a few clocks, an exchange through LDS a hundred):
+// within rows of 16 lanes by 1, 2, 4 and 8, then the last lane of a row to the next row, and of the lower half to the upper.
+template <int CTRL, int ROWS, typename V>
+__device__ __forceinline__ V lane_shift(V x, V none) {
+    constexpr int N = sizeof(V) / 4;
+    int from[N], to[N];
+    __builtin_memcpy(from, &x, sizeof(V));
+    __builtin_memcpy(to, &none, sizeof(V));
 #pragma unroll
-    for (int off = 32; off; off >>= 1) {
-        const V o = __shfl_xor(x, off);
-        x = o > x ? o : x;
-    }
+    for (int k = 0; k < N; ++k) to[k] = __builtin_amdgcn_update_dpp(to[k], from[k], CTRL, ROWS, 0xf, false);
+    V y;
+    __builtin_memcpy(&y, to, sizeof(V));
+    return y;
+}
+template <typename V, typename Op>
+__device__ __forceinline__ V wave_scan(V x, V none, Op op) {
+    x = op(x, lane_shift<0x111, 0xf>(x, none));      // row_shr 1, 2, 4, 8
+    x = op(x, lane_shift<0x112, 0xf>(x, none));
+    x = op(x, lane_shift<0x114, 0xf>(x, none));
+    x = op(x, lane_shift<0x118, 0xf>(x, none));
+    x = op(x, lane_shift<0x142, 0xa>(x, none));      // row_bcast 15 into rows 1 and 3
+    return op(x, lane_shift<0x143, 0xc>(x, none));   // row_bcast 31 into rows 2 and 3
+}
+template <typename V>
+__device__ __forceinline__ V last_lane(V x) {
+    constexpr int N = sizeof(V) / 4;
+    int w[N];
+    __builtin_memcpy(w, &x, sizeof(V));
+#pragma unroll
+    for (int k = 0; k < N; ++k) w[k] = __builtin_amdgcn_readlane(w[k], 63);
+    __builtin_memcpy(&x, w, sizeof(V));
     return x;
 }
 template <typename V>
-__device__ __forceinline__ V wave_sum(V x) {
-#pragma unroll
-    for (int off = 32; off; off >>= 1) x += __shfl_xor(x, off);
-    return x;
+__device__ __forceinline__ V wave_incl_scan(V x) {
+    return wave_scan(x, V(0), [](V p, V q) { return p + q; });
 }
 template <typename V>
-__device__ __forceinline__ V wave_incl_scan(V x, int lane) {
-#pragma unroll
-    for (int off = 1; off < 64; off <<= 1) {
-        const V up = __shfl_up(x, off);
-        if (lane >= off) x += up;
-    }
-    return x;
+__device__ __forceinline__ V wave_sum(V x) { return last_lane(wave_incl_scan(x)); }
+template <typename V>
+__device__ __forceinline__ V wave_max(V x) {      // (x itself in place of a lane that is not there: the maximum does not mind)
+    x = max(x, lane_shift<0x111, 0xf>(x, x));
+    x = max(x, lane_shift<0x112, 0xf>(x, x));
+    x = max(x, lane_shift<0x114, 0xf>(x, x));
+    x = max(x, lane_shift<0x118, 0xf>(x, x));
+    x = max(x, lane_shift<0x142, 0xa>(x, x));
+    return last_lane(max(x, lane_shift<0x143, 0xc>(x, x)));
 }
 
 // Over part[0, n) in LDS (entries >= 0), by one whole wavefront: the first positive entry whose inclusive prefix sum exceeds
@@ -185,9 +243,9 @@ __device__ __forceinline__ Found<V> find_prefix(const V* part, int n, int lane, 
         sum += part[i];
         if (part[i] > 0) last = i;
     }
-    const V incl = wave_incl_scan(sum, lane);
+    const V incl = wave_incl_scan(sum);
     Found<V> f;
-    f.total = __shfl(incl, 63);
+    f.total = last_lane(incl);
     const V target = target_of(f.total);
     const uint64_t over = __builtin_amdgcn_ballot_w64(incl > target && last >= 0);
     if (over) {
@@ -204,9 +262,7 @@ __device__ __forceinline__ Found<V> find_prefix(const V* part, int n, int lane, 
         f.at = __shfl(at, who);
         f.before = __shfl(before, who);
     } else {
-#pragma unroll
-        for (int off = 32; off; off >>= 1) last = max(last, __shfl_xor(last, off));
-        f.at = max(last, 0);
+        f.at = max(wave_max(last), 0);
         f.before = f.total;
     }
     return f;
@@ -215,15 +271,15 @@ __device__ __forceinline__ Found<V> find_prefix(const V* part, int n, int lane, 
 // One wavefront per block of 2048 logits, four blocks per workgroup.
 template <bool BF16>
 __global__ void __launch_bounds__(kThreads) k_sample_blocks(const SampleArgs a) {
+    touch_args<SampleArgs>();
     const int lane = threadIdx.x & 63;
-    const int row = blockIdx.x / a.wg_per_row;
-    const int blk = (blockIdx.x - row * a.wg_per_row) * (kThreads / 64) + __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
-    const int b = row / a.T, i = row - b * a.T;
+    const int row = a.div_wg.div((int)blockIdx.x);
+    const int blk = ((int)blockIdx.x - row * a.wg_per_row) * (kThreads / 64) + __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    const int b = a.div_T.div(row), i = row - b * a.T;
     if (blk >= a.n_blocks || (a.n_query && i >= a.n_query[b])) return;
     const SampleRow<BF16> logits(a, b, i);
     float x[4][8];
-#pragma unroll
-    for (int k = 0; k < 4; ++k) logits.load(blk * kSampleChunks + k * 64 + lane, x[k]);
+    logits.load_each(blk * kSampleChunks + lane, 64, x);
     const SampleRule rule = sample_rule(a, b);
     float m[4];
 #pragma unroll
@@ -247,11 +303,17 @@ __global__ void __launch_bounds__(kThreads) k_sample_blocks(const SampleArgs a) 
             for (int k = 0; k < 4; ++k)
 #pragma unroll
                 for (int j = 0; j < 8; ++j) part[k] += x[k][j] == M ? 1.0 : 0.0;
-        } else {
+        } else if (const double least = Md - 1000.0 / rule.c; least > -3e38 && fabs(Md) * rule.c < 3e8) {
+            // logits below it weigh less than 2^-980 (its rounding to 24 bits moves the exponent by less than 20): they count as that, and a
+            // sum of 1 or more does not notice
+            const float low = (float)least;
 #pragma unroll
             for (int j = 0; j < 8; ++j)
 #pragma unroll
-                for (int k = 0; k < 4; ++k) part[k] += exp2_64(((double)x[k][j] - Md) * rule.c);
+                for (int k = 0; k < 4; ++k) part[k] += exp2_64_normal((double)fmaxf(x[k][j], low) - Md, rule.c);
+        } else {           // (temperatures of 1e35 and more, and those below 1e-8 of the maximum)
+            for (int k = 0; k < 4; ++k)
+                for (int j = 0; j < 8; ++j) part[k] += exp2_64(((double)x[k][j] - Md) * rule.c);
         }
         sum = wave_sum((part[0] + part[1]) + (part[2] + part[3]));
     }
@@ -263,7 +325,7 @@ __global__ void __launch_bounds__(kThreads) k_sample_blocks(const SampleArgs a) 
 template <typename V>
 __device__ __forceinline__ V block_scan(V x, V* s_part, int tid, V& total) {
     const int lane = tid & 63, wave = tid >> 6;
-    const V incl = wave_incl_scan(x, lane);
+    const V incl = wave_incl_scan(x);
     if (lane == 63) s_part[wave] = incl;
     __syncthreads();
     V before = 0;
@@ -309,7 +371,8 @@ __global__ void __launch_bounds__(kSampleThreads) k_sample_pick(const SampleArgs
     static_assert(sizeof(s_sorted) == kSampleList * 4, "the chunks of the candidates lie where a bin is sorted later");
 
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int row = blockIdx.x, b = row / a.T, i = row - b * a.T;
+    touch_args<SampleArgs>();
+    const int row = blockIdx.x, b = a.div_T.div(row), i = row - b * a.T;
     int32_t* const token = a.tokens + row;
     float* const prob = a.probs ? a.probs + row : nullptr;
     if (a.n_query && i >= a.n_query[b]) {
@@ -341,11 +404,13 @@ __global__ void __launch_bounds__(kSampleThreads) k_sample_pick(const SampleArgs
             if ((float)blocks[k].max == mx) at = max(at, -k);
         at = -block_max(at, s_int, tid);
         int e = -0x7fffffff;
-        float x[8];
-        logits.load(at * kSampleChunks + tid, x);
+        if (tid < kSampleChunks) {
+            float x[8];
+            logits.load(at * kSampleChunks + tid, x);
 #pragma unroll
-        for (int j = 7; j >= 0; --j)
-            if (x[j] == mx) e = -(logits.first(at * kSampleChunks + tid) + j);
+            for (int j = 7; j >= 0; --j)
+                if (x[j] == mx) e = -(logits.first(at * kSampleChunks + tid) + j);
+        }
         e = -block_max(e, s_int, tid);
         if (tid == 0) {
             *token = e;
@@ -374,18 +439,15 @@ __global__ void __launch_bounds__(kSampleThreads) k_sample_pick(const SampleArgs
         const double target = (double)u * f.total;
         const bool past = u >= 1.f || f.before >= f.total;      // nothing exceeds the target: the last positive weight
         double w[32], sum = 0.0;
+        float x[4][8];
+        logits.load_each(f.at * kSampleChunks + lane * 4, 1, x);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            float x[8];
-            logits.load(f.at * kSampleChunks + lane * 4 + k, x);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                w[8 * k + j] = weight(x[j]);
-                sum += w[8 * k + j];
-            }
+        for (int j = 0; j < 32; ++j) {
+            w[j] = weight(x[j >> 3][j & 7]);
+            sum += w[j];
         }
         const int e0 = logits.first(f.at * kSampleChunks + lane * 4);
-        double run = f.before + wave_incl_scan(sum, lane) - sum, wf = 0.0;
+        double run = f.before + wave_incl_scan(sum) - sum, wf = 0.0;
         int found = -1, last = -1;
 #pragma unroll
         for (int j = 0; j < 32; ++j) {
@@ -414,15 +476,19 @@ __global__ void __launch_bounds__(kSampleThreads) k_sample_pick(const SampleArgs
     // ---- lo: a value that no kept entry lies below
     const uint16_t* maxima = a.maxima + (int64_t)row * a.n_blocks * kSampleChunks;
     const int n_groups8 = a.n_blocks * (kSampleChunks / 8);
-    auto each_max = [&](auto&& body) {       // body(iteration, chunk, upper half of its maximum's key); chunks in index order over (iteration, thread, call)
-        for (int it = 0; it * kSampleThreads < n_groups8; ++it) {
-            const int g = it * kSampleThreads + tid;
-            const u32x4 x = *reinterpret_cast<const u32x4*>(maxima + 8 * min(g, n_groups8 - 1));
-            if (g >= n_groups8) continue;
+    const int n_it = (n_groups8 + kSampleThreads - 1) / kSampleThreads;
+    // body(iteration, first of this thread's eight chunks, their eight halves); chunks are in index order over (iteration, thread).  Four
+    // iterations' loads are in flight at a time.
+    auto each_max = [&](auto&& body) {
+        for (int it0 = 0; it0 < n_it; it0 += 4) {
+            u32x4 x[4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                body(it, 8 * g + 2 * j, x[j] & 0xffffu);
-                body(it, 8 * g + 2 * j + 1, x[j] >> 16);
+            for (int k = 0; k < 4; ++k) x[k] = *reinterpret_cast<const u32x4*>(maxima + 8 * min((it0 + k) * kSampleThreads + tid, n_groups8 - 1));
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                if (it0 + k >= n_it) break;
+                const int g = (it0 + k) * kSampleThreads + tid;
+                body(it0 + k, 8 * g, g < n_groups8 ? x[k] : u32x4{0, 0, 0, 0});
             }
         }
     };
@@ -440,26 +506,39 @@ __global__ void __launch_bounds__(kSampleThreads) k_sample_pick(const SampleArgs
     const uint32_t lowest = order_key(-3.4028235e38f);      // (entries of -inf are never kept)
     uint32_t lo = lowest;
     if (rule.by_k) {
-        // the least of the maxima of up to 1024 groups of chunks: as many logits are as large; or that of all chunks
-        uint32_t least = 0xffffu, of_groups = 0xffffu, v[4] = {0, 0, 0, 0};
-        int groups = 0, chunks = 0, n_groups, n_chunks;
-        each_max([&](int, int c, uint32_t x) {
-            const bool any = x >= lowest >> 16;
-            chunks += any ? 1 : 0;
-            least = any ? min(least, x) : least;
+        // the least of the maxima of as many groups of chunks, or of all chunks: as many logits are as large
+        uint32_t v[4] = {0, 0, 0, 0};
+        each_max([&](int, int, u32x4 x) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) v[j] = (c >> 1 & 3) == j ? max(v[j], x) : v[j];
+            for (int j = 0; j < 4; ++j) v[j] = max(v[j], max(x[j] & 0xffffu, x[j] >> 16));
         });
+        if (rule.top_k <= kSampleThreads) {      // (larger groups, and a higher bound)
+            v[0] = max(max(v[0], v[1]), max(v[2], v[3]));
+            v[1] = v[2] = v[3] = 0;
+        }
+        int count = 0, n_held;
+        uint32_t least = 0xffffu;
 #pragma unroll
         for (int j = 0; j < 4; ++j)
             if (v[j] >= lowest >> 16) {
-                ++groups;
-                of_groups = min(of_groups, v[j]);
+                ++count;
+                least = min(least, v[j]);
             }
-        block_scan(groups, s_int, tid, n_groups);
-        block_scan(chunks, s_int, tid, n_chunks);
-        if (n_groups >= rule.top_k) lo = (uint32_t)(0xffff - block_max((int)(0xffffu - of_groups), s_int, tid)) << 16;
-        else if (n_chunks >= rule.top_k) lo = (uint32_t)(0xffff - block_max((int)(0xffffu - least), s_int, tid)) << 16;
+        block_scan(count, s_int, tid, n_held);
+        if (n_held < rule.top_k) {
+            count = 0;
+            least = 0xffffu;
+            each_max([&](int, int, u32x4 x) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const uint32_t half = j & 1 ? x[j >> 1] >> 16 : x[j >> 1] & 0xffffu;
+                    count += half >= lowest >> 16 ? 1 : 0;
+                    least = half >= lowest >> 16 ? min(least, half) : least;
+                }
+            });
+            block_scan(count, s_int, tid, n_held);
+        }
+        if (n_held >= rule.top_k) lo = (uint32_t)(0xffff - block_max((int)(0xffffu - least), s_int, tid)) << 16;
     } else if (rule.by_p) {
         // entries of weight below (1 - p) Z / V hold less than (1 - p) Z together
         const double least = (1.0 - (double)rule.top_p) * (1.0 - 1e-9) * total / (double)a.V;
@@ -469,14 +548,12 @@ __global__ void __launch_bounds__(kSampleThreads) k_sample_pick(const SampleArgs
     if (rule.by_m && !rule.by_p) lo = max(lo, tau_m);
     lo = max(lo, lowest);
 
-    // ---- bins of equal width from the maximum down to lo
-    const float width = mx - key_value(lo);
-    const float inv = width > 0.f && width < INFINITY ? (float)kSampleBins / width : 0.f;
-    auto bin_of = [&](float x) { return x == mx ? 0 : min(kSampleBins - 1, (int)((mx - x) * inv)); };
     auto mass = [&](uint32_t k) { return (unsigned long long)(weight(key_value(k)) * a.mass_scale + 0.5); };
     auto clear_bins = [&] {
-        s_mass[tid] = 0;
-        s_count[tid] = 0;
+        if (tid < kSampleBins) {
+            s_mass[tid] = 0;
+            s_count[tid] = 0;
+        }
         __syncthreads();
     };
     // The first bin up to which the entries number `n` or more, or weigh `m` or more (the last one that holds any, if none does).
@@ -493,8 +570,8 @@ __global__ void __launch_bounds__(kSampleThreads) k_sample_pick(const SampleArgs
                 cs += c[j];
                 ws += w[j];
             }
-            const uint32_t ci = wave_incl_scan(cs, lane);
-            const unsigned long long wi = wave_incl_scan(ws, lane);
+            const uint32_t ci = wave_incl_scan(cs);
+            const unsigned long long wi = wave_incl_scan(ws);
             const uint64_t reached = __builtin_amdgcn_ballot_w64(cs > 0 && (by_mass ? (double)wi >= m : ci >= n));
             const uint64_t some = __builtin_amdgcn_ballot_w64(cs > 0);
             const int who = reached ? (int)__builtin_ctzll(reached) : 63 - (int)__builtin_clzll(some | 1ull);
@@ -518,122 +595,173 @@ __global__ void __launch_bounds__(kSampleThreads) k_sample_pick(const SampleArgs
         __syncthreads();
         return s_bin;
     };
-    // First over the chunks' maxima (their lower ends): where these alone suffice, nothing beyond that bin is kept.
-    int last_bin = kSampleBins - 1;
-    if (rule.by_k || rule.by_p) {
-        clear_bins();
-        each_max([&](int, int, uint32_t x) {
-            const uint32_t key = x << 16;
-            if (key < lo) return;
-            const int at = bin_of(key_value(key));
-            atomicAdd(&s_count[at], 1u);
-            if (!rule.by_k) atomicAdd(&s_mass[at], mass(key));
-        });
-        const BinFound f = find_bin(!rule.by_k, (uint32_t)rule.top_k, (double)rule.top_p * (1.0 + 1e-9) * total * a.mass_scale);
-        if (f.reached) last_bin = f.bin;
-    }
-
-    // ---- the candidates, in index order: chunks that may hold one (by the upper ends of their maxima), then the logits
+    // ---- the candidates, in index order.  First chunks whose maximum (its upper half's upper end) reaches a bound, then their logits.
     uint64_t* s_list = reinterpret_cast<uint64_t*>(s_mem);
     uint32_t* s_chunk = reinterpret_cast<uint32_t*>(s_sorted);
-    auto may_hold = [&](uint32_t half) {
-        const uint32_t key = half << 16 | 0xffffu;
-        return key >= lo && (key >= order_key(mx) || bin_of(key_value(key)) <= last_bin);
-    };
-    auto hits_of = [&](int it) {             // of this thread's eight chunks of an iteration
-        const int g = it * kSampleThreads + tid;
-        uint32_t hits = 0;
-        if (g < n_groups8) {
-            const u32x4 x = *reinterpret_cast<const u32x4*>(maxima + 8 * g);
+    // how many chunks' halves reach `half`; (half, chunk) of each to s_list if they fit
+    auto list_chunks = [&](uint32_t half) {
+        // counts by (iteration, wavefront), their prefix sums, then the places
+        uint32_t* s_hits = s_chunk;
+        auto hits_of = [&](u32x4 x) {            // of eight chunks
+            uint32_t hits = 0;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) hits |= (may_hold(x[j] & 0xffffu) ? 1u : 0u) << (2 * j) | (may_hold(x[j] >> 16) ? 2u : 0u) << (2 * j);
-        }
-        return hits;
-    };
-    auto count_before = [&](uint32_t hits, int& all) {      // hits of the wavefront's lanes before this one, and of all
-        const uint32_t c = (uint32_t)__builtin_popcount(hits);
-        int before = 0;
-        all = 0;
+            for (int j = 0; j < 4; ++j) hits |= ((x[j] & 0xffffu) >= half ? 1u : 0u) << (2 * j) | ((x[j] >> 16) >= half ? 2u : 0u) << (2 * j);
+            return hits;
+        };
+        auto count_before = [&](uint32_t hits, int& all) {      // hits of the wavefront's lanes before this one, and of all
+            const uint32_t c = (uint32_t)__builtin_popcount(hits);
+            int before = 0;
+            all = 0;
 #pragma unroll
-        for (int bit = 0; bit < 4; ++bit) {
-            const uint64_t m = __builtin_amdgcn_ballot_w64(c >> bit & 1u);
-            before += (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0u)) << bit;
-            all += __builtin_popcountll(m) << bit;
-        }
-        return before;
-    };
-    int n_hit = 0, n = 0;
-    {
-        // hits by (iteration, wavefront), their prefix sums, then the places
-        uint32_t* s_hits = reinterpret_cast<uint32_t*>(s_mem);
-        const int n_it = (n_groups8 + kSampleThreads - 1) / kSampleThreads;
-        for (int it = 0; it < n_it; ++it) {
-            int all;
-            count_before(hits_of(it), all);
+            for (int bit = 0; bit < 4; ++bit) {
+                const uint64_t m = __builtin_amdgcn_ballot_w64(c >> bit & 1u);
+                before += (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0u)) << bit;
+                all += __builtin_popcountll(m) << bit;
+            }
+            return before;
+        };
+        int n_hit, all;
+        __syncthreads();
+        each_max([&](int it, int, u32x4 x) {
+            count_before(hits_of(x), all);
             if (lane == 0) s_hits[it * kSampleWaves + wave] = (uint32_t)all;
-        }
+        });
         __syncthreads();
         const int per = (n_it * kSampleWaves + kSampleThreads - 1) / kSampleThreads;
-        uint32_t sum = 0;
-        for (int k = tid * per; k < min(n_it * kSampleWaves, (tid + 1) * per); ++k) sum += s_hits[k];
-        int at = block_scan((int)sum, s_int, tid, n_hit);
+        int sum = 0;
+        for (int k = tid * per; k < min(n_it * kSampleWaves, (tid + 1) * per); ++k) sum += (int)s_hits[k];
+        int at = block_scan(sum, s_int, tid, n_hit);
+        if (n_hit > kSampleList) return n_hit;
         for (int k = tid * per; k < min(n_it * kSampleWaves, (tid + 1) * per); ++k) {
             const int c = (int)s_hits[k];
             s_hits[k] = (uint32_t)at;
             at += c;
         }
         __syncthreads();
-        if (n_hit <= kSampleList)
-            for (int it = 0; it < n_it; ++it) {
-                int all;
-                const uint32_t hits = hits_of(it);
-                int to = (int)s_hits[it * kSampleWaves + wave] + count_before(hits, all);
-                for (uint32_t rest = hits; rest; rest &= rest - 1) s_chunk[to++] = 8 * (it * kSampleThreads + tid) + __builtin_ctz(rest);
-            }
-        __syncthreads();
-    }
-    bool listed = n_hit <= kSampleList;
-    auto candidate = [&](float x) { return order_key(x) >= lo && bin_of(x) <= last_bin; };
-    if (listed) {
-        const int q = (n_hit + kSampleThreads - 1) / kSampleThreads, h0 = min(n_hit, tid * q), h1 = min(n_hit, h0 + q);
-        int mine = 0;
-        float x[8];
-        for (int h = h0; h < h1; ++h) {
-            logits.load((int)s_chunk[h], x);
+        each_max([&](int it, int c, u32x4 x) {
+            const uint32_t hits = hits_of(x);
+            int to = (int)s_hits[it * kSampleWaves + wave] + count_before(hits, all);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) mine += candidate(x[j]) ? 1 : 0;
+            for (int j = 0; j < 8; ++j)
+                if (hits >> j & 1u) s_list[to++] = (uint64_t)(j & 1 ? x[j >> 1] >> 16 : x[j >> 1] & 0xffffu) << 32 | (uint32_t)(c + j);
+        });
+        __syncthreads();
+        return n_hit;
+    };
+    // Of these, by bins of equal width in halves from the maximum's down: where the chunks' maxima alone (their lower ends) suffice,
+    // nothing beyond that bin is kept.
+    const uint32_t top_half = order_key(mx) >> 16;
+    uint32_t half = lo >> 16;
+    int n_hit = list_chunks(half);
+    if (rule.by_k || rule.by_p) {
+        int shift = 0;
+        while ((top_half - half) >> shift >= kSampleBins) ++shift;
+        clear_bins();
+        auto count = [&](uint32_t h) {
+            if (h << 16 < lo) return;
+            const uint32_t at = (top_half - h) >> shift;
+            atomicAdd(&s_count[at], 1u);
+            if (!rule.by_k) atomicAdd(&s_mass[at], mass(h << 16));
+        };
+        if (n_hit <= kSampleList) {
+            for (int l = tid; l < n_hit; l += kSampleThreads) count((uint32_t)(s_list[l] >> 32));
+        } else {
+            each_max([&](int, int, u32x4 x) {
+#pragma unroll 1
+                for (int j = 0; j < 8; ++j) {
+                    count(x[0] & 0xffffu);
+                    x = u32x4{__builtin_amdgcn_alignbit(x[1], x[0], 16), __builtin_amdgcn_alignbit(x[2], x[1], 16), __builtin_amdgcn_alignbit(x[3], x[2], 16), x[3] >> 16};
+                }
+            });
         }
-        int at = block_scan(mine, s_int, tid, n);
-        listed = n <= kSampleList;
-        if (listed)
-            for (int h = h0; h < h1; ++h) {
-                if (q > 1) logits.load((int)s_chunk[h], x);
-                const int e0 = logits.first((int)s_chunk[h]);
+        const BinFound f = find_bin(!rule.by_k, (uint32_t)rule.top_k, (double)rule.top_p * (1.0 + 1e-9) * total * a.mass_scale);
+        if (f.reached) {
+            const uint32_t edge = top_half + 1 - ((uint32_t)(f.bin + 1) << shift);      // (bins up to it hold the halves from here on)
+            if ((uint32_t)(f.bin + 1) << shift <= top_half) half = max(half, edge);
+            lo = max(lo, half << 16);
+        }
+    }
+    if (n_hit > kSampleList) n_hit = list_chunks(half);
+    bool listed = n_hit <= kSampleList;
+    int n = 0;
+    if (listed) {
+        // those that remain, to s_chunk
+        int q = (n_hit + kSampleThreads - 1) / kSampleThreads, h0 = min(n_hit, tid * q), h1 = min(n_hit, h0 + q), mine = 0;
+        for (int h = h0; h < h1; ++h) mine += (uint32_t)(s_list[h] >> 32) >= half ? 1 : 0;
+        int all, at = block_scan(mine, s_int, tid, all);
+        for (int h = h0; h < h1; ++h)
+            if ((uint32_t)(s_list[h] >> 32) >= half) s_chunk[at++] = (uint32_t)s_list[h];
+        n_hit = all;
+        __syncthreads();
+        // their logits: up to eight chunks of a thread stay in registers between counting and listing
+        constexpr int HOLD = 8;
+        q = (n_hit + kSampleThreads - 1) / kSampleThreads;
+        h0 = min(n_hit, tid * q);
+        h1 = min(n_hit, h0 + q);
+        typename SampleRow<BF16>::Raw raw[HOLD];
+        int c[HOLD];
+        auto fetch = [&](int h) {
+#pragma unroll
+            for (int k = 0; k < HOLD; ++k) {
+                if (k >= q) break;         // (uniform)
+                c[k] = h + k < h1 ? (int)s_chunk[h + k] : -1;
+                raw[k] = logits.fetch(c[k]);
+            }
+        };
+        auto each_logit = [&](auto&& body) {
+#pragma unroll
+            for (int k = 0; k < HOLD; ++k) {
+                if (k >= q) break;
+                if (c[k] < 0) continue;
+                float x[8];
+                logits.unpack(c[k], raw[k], x);
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
-                    if (candidate(x[j])) s_list[at++] = list_entry(order_key(x[j]), e0 + j);
+                    if (order_key(x[j]) >= lo) body(order_key(x[j]), logits.first(c[k]) + j);
+            }
+        };
+        mine = 0;
+        for (int h = h0; h < h1; h += HOLD) {
+            fetch(h);
+            each_logit([&](uint32_t, int) { ++mine; });
+        }
+        at = block_scan(mine, s_int, tid, n);
+        listed = n <= kSampleList;
+        if (listed)
+            for (int h = h0; h < h1; h += HOLD) {
+                if (q > HOLD) fetch(h);
+                each_logit([&](uint32_t key, int e) { s_list[at++] = list_entry(key, e); });
             }
         __syncthreads();
     }
+
+    // ---- bins of equal width from the maximum down to lo, which the candidates reach
+    const float width = mx - key_value(lo);
+    const float inv = width > 0.f && width < INFINITY ? (float)kSampleBins / width : 0.f;
+    auto bin_of = [&](float x) { return x == mx ? 0 : min(kSampleBins - 1, (int)((mx - x) * inv)); };
     const int q = (n + kSampleThreads - 1) / kSampleThreads, l0 = min(n, tid * q), l1 = min(n, l0 + q);     // this thread's entries
     uint64_t last_kept = 0;             // the last entry that is kept
     if (listed && (rule.by_k || rule.by_p)) {
         // ---- the exact threshold: a histogram of the list, and the entries of the bin in which it falls in order
-        clear_bins();
-        for (int l = l0; l < l1; ++l) {
-            const uint32_t key = (uint32_t)(s_list[l] >> 32);
-            const int at = bin_of(key_value(key));
-            atomicAdd(&s_count[at], 1u);
-            if (rule.by_p) atomicAdd(&s_mass[at], mass(key));
+        const bool whole = n <= 64;          // one wavefront's sort takes the whole list
+        if (!whole) {
+            clear_bins();
+            for (int l = l0; l < l1; ++l) {
+                const uint32_t key = (uint32_t)(s_list[l] >> 32);
+                const int at = bin_of(key_value(key));
+                atomicAdd(&s_count[at], 1u);
+                if (rule.by_p) atomicAdd(&s_mass[at], mass(key));
+            }
         }
+        const BinFound all_of_it{0, 1, 0u, 0ull};
         // the entries of a bin into s_sorted, descending; how many
         auto sort_bin = [&](int bin) {
             int mine = 0, m;
-            for (int l = l0; l < l1; ++l) mine += bin_of(entry_value(s_list[l])) == bin ? 1 : 0;
+            for (int l = l0; l < l1; ++l) mine += whole || bin_of(entry_value(s_list[l])) == bin ? 1 : 0;
             int at = block_scan(mine, s_int, tid, m);
             if (m > kSampleSort) return m;
             for (int l = l0; l < l1; ++l)
-                if (bin_of(entry_value(s_list[l])) == bin) s_sorted[at++] = s_list[l];
+                if (whole || bin_of(entry_value(s_list[l])) == bin) s_sorted[at++] = s_list[l];
             int size = 64;
             while (size < m) size *= 2;
             for (int k = m + tid; k < size; k += kSampleThreads) s_sorted[k] = 0ull;
@@ -685,7 +813,7 @@ __global__ void __launch_bounds__(kSampleThreads) k_sample_pick(const SampleArgs
         double target = (double)rule.top_p * total * a.mass_scale;
         bool done = false;
         if (rule.by_k) {
-            const BinFound f = find_bin(false, (uint32_t)rule.top_k, 0.0);
+            const BinFound f = whole ? all_of_it : find_bin(false, (uint32_t)rule.top_k, 0.0);
             const int m = sort_bin(f.bin);
             listed = m <= kSampleSort;
             if (listed) {
@@ -703,7 +831,7 @@ __global__ void __launch_bounds__(kSampleThreads) k_sample_pick(const SampleArgs
             }
         }
         if (rule.by_p && listed && !done) {
-            const BinFound f = find_bin(true, 0u, target);
+            const BinFound f = whole ? all_of_it : find_bin(true, 0u, target);
             const int m = sort_bin(f.bin);
             listed = m <= kSampleSort;
             if (listed) {
@@ -748,8 +876,7 @@ __global__ void __launch_bounds__(kSampleThreads) k_sample_pick(const SampleArgs
     auto each = [&](auto&& body) {       // body(iteration, first element of the chunk, its eight values)
         for (int it = 0; it < iters; it += 4) {
             float x[4][8];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) logits.load((it + k) * kSampleThreads + tid, x[k]);
+            logits.load_each(it * kSampleThreads + tid, kSampleThreads, x);
 #pragma unroll
             for (int k = 0; k < 4; ++k)
                 if (it + k < iters) body(it + k, logits.first((it + k) * kSampleThreads + tid), x[k]);
@@ -766,7 +893,7 @@ __global__ void __launch_bounds__(kSampleThreads) k_sample_pick(const SampleArgs
                 h[j] = s_hist[255 - (4 * lane + j)];
                 sum += h[j];
             }
-            const unsigned long long incl = wave_incl_scan(sum, lane) + above;
+            const unsigned long long incl = wave_incl_scan(sum) + above;
             const uint64_t reached = __builtin_amdgcn_ballot_w64((double)incl >= target && sum > 0);
             // rounding of the target can leave nothing that reaches it: then the lowest digit that holds something
             const uint64_t any = __builtin_amdgcn_ballot_w64(sum > 0);
@@ -870,7 +997,7 @@ __global__ void __launch_bounds__(kSampleThreads) k_sample_pick(const SampleArgs
             uint32_t mine = 0;
 #pragma unroll
             for (int j = 0; j < 8; ++j) mine += order_key(x[j]) == tau ? 1u : 0u;
-            uint32_t run = f.before + wave_incl_scan(mine, lane) - mine;
+            uint32_t run = f.before + wave_incl_scan(mine) - mine;
             int found = -1;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
@@ -912,7 +1039,7 @@ __global__ void __launch_bounds__(kSampleThreads) k_sample_pick(const SampleArgs
         w[j] = kept(x[j], 8 * c - logits.shift + j) ? weight(x[j]) : 0.0;
         sum += w[j];
     }
-    double run = f.before + wave_incl_scan(sum, lane) - sum;
+    double run = f.before + wave_incl_scan(sum) - sum;
     const bool past = u >= 1.f || f.before >= f.total;          // nothing exceeds the target: the last positive weight
     int found = -1, last = -1;
     double wf = 0.0, wl = 0.0;

@@ -320,6 +320,8 @@ int ssv_sample(const void* logits, const float* temperature, const int32_t* top_
     a.T = p->T; a.V = p->V;
     a.n_blocks = sample_blocks(p->V);
     a.wg_per_row = ceil_div(a.n_blocks, kThreads / 64);
+    a.div_wg = FastDiv::of(a.wg_per_row);
+    a.div_T = FastDiv::of(p->T);
     int bits = 0;
     while ((1 << bits) < p->V) ++bits;
     a.mass_scale = std::ldexp(1.0, 62 - bits);
