@@ -16,7 +16,7 @@
 
 namespace ssv {
 
-struct SampleBlock { double sum, max; };     // of 2048 logits: sum of 2^((x - max) log2(e) / t), maximum
+struct SampleBlock { double sum, max; };     // of 2048 logits: sum of 2^(x c - e), c = log2(e) / t, e the whole number next to max c; maximum
 
 struct SampleArgs {
     const char* logits;
@@ -70,32 +70,40 @@ __device__ __forceinline__ double exp2_64(double y) {
     return __builtin_ldexp(p, (int)n);
 }
 
-// The same for y = d c, d <= 0 and d c >= -1000, without the slow conversions: adding 1.5 * 2^52 rounds to a whole number and leaves it in
-// the low bits, from where it goes into the exponent.
-__device__ __forceinline__ double exp2_64_normal(double d, double c) {
-    const double magic = 6755399441055744.0;
-    const double t = __builtin_fma(d, c, magic), f = __builtin_fma(d, c, magic - t);
-    double p = 7.072585949269223e-09;
-    p = __builtin_fma(p, f, 1.0208690299958306e-07);
-    p = __builtin_fma(p, f, 1.321544258792169e-06);
-    p = __builtin_fma(p, f, 1.5252657260200837e-05);
-    p = __builtin_fma(p, f, 0.0001540353044173605);
-    p = __builtin_fma(p, f, 0.0013333558230164974);
-    p = __builtin_fma(p, f, 0.009618129107606888);
-    p = __builtin_fma(p, f, 0.05550410866444772);
-    p = __builtin_fma(p, f, 0.24022650695910097);
-    p = __builtin_fma(p, f, 0.69314718055995);
+// 2^(x c - e) for a whole number e, x c - e in [-1000, 1000], for sums over blocks: degree 8 (off by 1.1e-12 at most: such a shift of the
+// running sum moves a token in one of a million samples of the largest vocabulary), and without slow conversions: adding
+// 1.5 * 2^52 - e rounds to a whole number and leaves it in the low bits, from where it goes into the exponent.
+__device__ __forceinline__ double exp2_64_from(double x, double c, double magic_e) {
+    const double t = __builtin_fma(x, c, magic_e), f = __builtin_fma(x, c, magic_e - t);
+    double p = 1.3255224878668817e-06;
+    p = __builtin_fma(p, f, 1.5310079402249296e-05);
+    p = __builtin_fma(p, f, 0.00015403455852453838);
+    p = __builtin_fma(p, f, 0.0013333450568000645);
+    p = __builtin_fma(p, f, 0.009618129159402558);
+    p = __builtin_fma(p, f, 0.05550410941205933);
+    p = __builtin_fma(p, f, 0.2402265069581299);
+    p = __builtin_fma(p, f, 0.6931471805459335);
     p = __builtin_fma(p, f, 1.0);
     const uint64_t bits = __builtin_bit_cast(uint64_t, p);
     const uint32_t n = (uint32_t)__builtin_bit_cast(uint64_t, t);
     return __builtin_bit_cast(double, (uint64_t)((uint32_t)(bits >> 32) + (n << 20)) << 32 | (uint32_t)bits);
 }
 
+// Whether 2^(x c - e) is within reach for a block of maximum M: not for temperatures of 1e35 and more, nor those below 1e-8 of the
+// maximum (nor M = +-inf); such blocks sum 2^((x - M) c).
+__device__ __forceinline__ bool whole_exponents(double M, double c) { return M - 1000.0 / c > -3e38 && fabs(M) * c < 3e8; }
+
 // Weight of a logit against a maximum; 1 at the maximum, whatever that is.
 struct SampleWeight {
     double M, c;       // c = log2(e) / temperature
     float Mf;
     __device__ __forceinline__ double operator()(float x) const { return x == Mf ? 1.0 : exp2_64(((double)x - M) * c); }
+    // of a block of sum 1
+    __device__ __forceinline__ double of_block(double max) const {
+        if (!whole_exponents(max, c)) return (*this)((float)max);
+        const double e = __builtin_rint(max * c);
+        return whole_exponents(M, c) ? exp2_64((e - M * c)) : exp2_64((max - M) * c + (e - max * c));
+    }
 };
 
 // The settings of a sequence as the header reads them.
@@ -150,6 +158,7 @@ struct SampleRow {
         }
         return r;
     }
+    template <bool CLEAN = true>
     __device__ __forceinline__ void unpack(int c, const Raw& r, float (&x)[8]) const {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
@@ -168,16 +177,16 @@ struct SampleRow {
             }
         }
 #pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = clean(x[j]);
+        for (int j = 0; j < 8; ++j) x[j] = CLEAN ? clean(x[j]) : x[j] + 0.f;      // (either way no signalling NaN)
     }
     __device__ __forceinline__ void load(int c, float (&x)[8]) const { unpack(c, fetch(c), x); }
-    template <int N>
+    template <bool CLEAN = true, int N>
     __device__ __forceinline__ void load_each(int c, int step, float (&x)[N][8]) const {      // chunks c, c + step, ...
         Raw r[N];
 #pragma unroll
         for (int k = 0; k < N; ++k) r[k] = fetch(c + k * step);
 #pragma unroll
-        for (int k = 0; k < N; ++k) unpack(c + k * step, r[k], x[k]);
+        for (int k = 0; k < N; ++k) unpack<CLEAN>(c + k * step, r[k], x[k]);
     }
 };
 
@@ -279,14 +288,15 @@ __global__ void __launch_bounds__(kThreads) k_sample_blocks(const SampleArgs a) 
     if (blk >= a.n_blocks || (a.n_query && i >= a.n_query[b])) return;
     const SampleRow<BF16> logits(a, b, i);
     float x[4][8];
-    logits.load_each(blk * kSampleChunks + lane, 64, x);
+    logits.template load_each<false>(blk * kSampleChunks + lane, 64, x);       // (a maximum passes over NaN)
     const SampleRule rule = sample_rule(a, b);
     float m[4];
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-        m[k] = x[k][0];
+        m[k] = -INFINITY;
 #pragma unroll
-        for (int j = 1; j < 8; ++j) m[k] = fmaxf(m[k], x[k][j]);
+        for (int j = 0; j < 8; ++j) m[k] = fmaxf(m[k], x[k][j]);
+        m[k] += 0.f;
     }
     const float M = wave_max(fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])));
     if (rule.filters()) {
@@ -303,17 +313,20 @@ __global__ void __launch_bounds__(kThreads) k_sample_blocks(const SampleArgs a) 
             for (int k = 0; k < 4; ++k)
 #pragma unroll
                 for (int j = 0; j < 8; ++j) part[k] += x[k][j] == M ? 1.0 : 0.0;
-        } else if (const double least = Md - 1000.0 / rule.c; least > -3e38 && fabs(Md) * rule.c < 3e8) {
-            // logits below it weigh less than 2^-980 (its rounding to 24 bits moves the exponent by less than 20): they count as that, and a
-            // sum of 1 or more does not notice
-            const float low = (float)least;
+        } else if (whole_exponents(Md, rule.c)) {
+            // logits below M - 1000 / c weigh less than 2^-980 (the rounding of this bound to 24 bits moves the exponent by less than 20):
+            // they count as that, and a sum of 1/2 or more does not notice
+            const float low = (float)(Md - 1000.0 / rule.c);
+            const double magic_e = 6755399441055744.0 - __builtin_rint(Md * rule.c);
 #pragma unroll
             for (int j = 0; j < 8; ++j)
 #pragma unroll
-                for (int k = 0; k < 4; ++k) part[k] += exp2_64_normal((double)fmaxf(x[k][j], low) - Md, rule.c);
-        } else {           // (temperatures of 1e35 and more, and those below 1e-8 of the maximum)
-            for (int k = 0; k < 4; ++k)
-                for (int j = 0; j < 8; ++j) part[k] += exp2_64(((double)x[k][j] - Md) * rule.c);
+                for (int k = 0; k < 4; ++k) part[k] += exp2_64_from((double)fmaxf(x[k][j], low), rule.c, magic_e);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) part[k] += x[k][j] == M ? 1.0 : exp2_64(((double)x[k][j] - Md) * rule.c);
         }
         sum = wave_sum((part[0] + part[1]) + (part[2] + part[3]));
     }
@@ -427,7 +440,7 @@ __global__ void __launch_bounds__(kSampleThreads) k_sample_pick(const SampleArgs
         double sum = 0.0;
         for (int k = tid; k < a.n_blocks; k += kSampleThreads) {
             const SampleBlock x = blocks[k];
-            const double v = x.sum == 0.0 ? 0.0 : x.sum * weight((float)x.max);
+            const double v = x.sum == 0.0 ? 0.0 : x.sum * weight.of_block(x.max);
             s_sum[k] = v;
             sum += v;
         }
