@@ -25,6 +25,7 @@ struct PrefixPart {
     int rows, n_rg;                    // rows per (cache, KV head); groups of them, one per workgroup
     int max_len;
     int n_slices, slot0;               // slices per pair, and the first one's partial-state slot
+    FastDiv div_rg, div_slices;
     int n_wg, n_pad;                   // workgroups, and the same rounded up to a multiple of 8
     int64_t k_s[3], v_s[3];            // bytes: cache, KV head, row
 };
@@ -37,14 +38,14 @@ struct PrefixArgs {
     int T, H, H_kv, H_g;
     float scale_log2;
     int64_t rows_total;
-    FastDiv div_TH, div_Hg;
+    FastDiv div_TH, div_Hg, div_Hkv;
     int64_t q_s[3];                    // bytes: sequence, node, head
 };
 
 constexpr int kPrefixThreads = 512;
 constexpr int kPrefixWaves = kPrefixThreads / 64;
 constexpr int kPrefixStep = 32;        // keys per step of a wavefront on the keys path
-constexpr int kPrefixMaxSlots = 64;    // partial states per row
+constexpr int kPrefixMaxSlots = 128;   // partial states per row
 constexpr int kPrefixMinTiles = 2;     // tiles of 64 keys that a slice holds at least
 constexpr float kPrefixRaiseLog2 = 8.f;   // the reference maximum follows the running one at a distance of up to 2^8
 
@@ -93,45 +94,54 @@ __device__ __forceinline__ float add_bf16_pair(uint32_t pair, float sum) {
     return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pair), __builtin_bit_cast(bf16x2, 0x3f803f80u), sum, false);
 }
 
-// What a workgroup of either path works on.
+// What a workgroup of either path works on: its place in the launch, and what the lengths make of it.  The place gives the
+// addresses of the queries, which are fetched while the lengths are on their way.
+struct PrefixPlace { int rg, slice, cache, g; };
+template <bool OWN>
+__device__ __forceinline__ PrefixPlace prefix_place(const PrefixArgs& a, int wg) {
+    const PrefixPart& pt = a.part[OWN];
+    PrefixPlace w;
+    const int ps = pt.div_rg.div(wg);                      // neighbours read the same keys
+    w.rg = wg - ps * pt.n_rg;
+    const int pair = pt.div_slices.div(ps);
+    w.slice = ps - pair * pt.n_slices;
+    w.cache = a.div_Hkv.div(pair);
+    w.g = pair - w.cache * a.H_kv;
+    return w;
+}
 struct PrefixWork {
-    int rg, slice, cache, g;
     int len, Tq, n_keys;               // Tq: nodes of the sequence (own caches only)
     int t0, t1;                        // tiles of 64 keys
 };
 template <bool OWN>
-__device__ __forceinline__ PrefixWork prefix_work(const PrefixArgs& a, int wg) {
+__device__ __forceinline__ PrefixWork prefix_work(const PrefixArgs& a, const PrefixPlace& at) {
     const PrefixPart& pt = a.part[OWN];
     PrefixWork w;
-    w.rg = wg % pt.n_rg;                                   // neighbours read the same keys
-    const int ps = wg / pt.n_rg;
-    w.slice = ps % pt.n_slices;
-    const int pair = ps / pt.n_slices;
-    w.cache = pair / a.H_kv;
-    w.g = pair - w.cache * a.H_kv;
-    w.len = min(max(pt.lens[w.cache], 0), pt.max_len);
-    w.Tq = OWN ? (a.n_query ? min(max(a.n_query[w.cache], 0), a.T) : a.T) : 0;
+    w.len = min(max(pt.lens[at.cache], 0), pt.max_len);
+    w.Tq = OWN ? (a.n_query ? min(max(a.n_query[at.cache], 0), a.T) : a.T) : 0;
     w.n_keys = w.len + w.Tq;
     const int n_tiles = (w.n_keys + kTile - 1) / kTile;
-    const int chunk = max((n_tiles + pt.n_slices - 1) / pt.n_slices, kPrefixMinTiles);
-    w.t0 = min(n_tiles, w.slice * chunk);
+    const int chunk = max(pt.div_slices.div(n_tiles + pt.n_slices - 1), kPrefixMinTiles);
+    w.t0 = min(n_tiles, at.slice * chunk);
     w.t1 = min(n_tiles, w.t0 + chunk);
     return w;
 }
 
-// Row r of a (cache, KV head): its sequence, node and head, and whether it exists.
-struct PrefixRow { int b, i, h; bool valid; };
+// Row r of a (cache, KV head): its sequence, node and head; and whether it exists.
+struct PrefixRow { int b, i, h; };
 template <bool OWN>
-__device__ __forceinline__ PrefixRow prefix_row(const PrefixArgs& a, const PrefixWork& w, int r) {
-    const PrefixPart& pt = a.part[OWN];
-    const int rc = min(r, pt.rows - 1);
+__device__ __forceinline__ PrefixRow prefix_row(const PrefixArgs& a, const PrefixPlace& at, int r) {
+    const int rc = min(r, a.part[OWN].rows - 1);
     const int bl = OWN ? 0 : a.div_TH.div(rc), in = rc - bl * a.T * a.H_g;
     PrefixRow x;
     x.i = a.div_Hg.div(in);
-    x.h = w.g * a.H_g + in - x.i * a.H_g;
-    x.b = w.cache * pt.per + bl;
-    x.valid = r < pt.rows && x.i < (OWN ? w.Tq : (a.n_query ? a.n_query[x.b] : a.T));
+    x.h = at.g * a.H_g + in - x.i * a.H_g;
+    x.b = at.cache * a.part[OWN].per + bl;
     return x;
+}
+template <bool OWN>
+__device__ __forceinline__ bool prefix_row_exists(const PrefixArgs& a, const PrefixWork& w, const PrefixRow& x, int r) {
+    return r < a.part[OWN].rows && x.i < (OWN ? w.Tq : (a.n_query ? a.n_query[x.b] : a.T));
 }
 __device__ __forceinline__ int64_t prefix_state_row(const PrefixArgs& a, const PrefixRow& x) { return ((int64_t)x.b * a.T + x.i) * a.H + x.h; }
 
@@ -161,27 +171,24 @@ __device__ __forceinline__ void prefix_keys(const PrefixArgs& a, int wg, char* s
     const PrefixPart& pt = a.part[OWN];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int n = lane & 15, G = lane >> 4;
-    const PrefixWork w = prefix_work<OWN>(a, wg);
-
     // ---- rows
+    const PrefixPlace place = prefix_place<OWN>(a, wg);
     PrefixRow row[RB];
     u32x4 qf[RB][KC];
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
-        row[rb] = prefix_row<OWN>(a, w, (w.rg * RB + rb) * 16 + n);
+        row[rb] = prefix_row<OWN>(a, place, (place.rg * RB + rb) * 16 + n);
         const char* qp = a.q + row[rb].b * a.q_s[0] + row[rb].i * a.q_s[1] + row[rb].h * a.q_s[2] + G * 16;
 #pragma unroll
         for (int c = 0; c < KC; ++c) qf[rb][c] = *reinterpret_cast<const u32x4*>(qp + c * 64);
-        if (!row[rb].valid) {
-#pragma unroll
-            for (int c = 0; c < KC; ++c) qf[rb][c] = u32x4{0, 0, 0, 0};
-        }
     }
+    __builtin_amdgcn_sched_barrier(0);
+    const PrefixWork w = prefix_work<OWN>(a, place);
 
     // ---- this slice's steps
     const int t0 = w.t0 * (kTile / kPrefixStep), t1 = min(w.t1 * (kTile / kPrefixStep), (w.n_keys + kPrefixStep - 1) / kPrefixStep);
-    const char* kbase = pt.k + w.cache * pt.k_s[0] + w.g * pt.k_s[1] + G * 16;
-    const char* vbase = pt.v + w.cache * pt.v_s[0] + w.g * pt.v_s[1] + n * (CW * ES);
+    const char* kbase = pt.k + place.cache * pt.k_s[0] + place.g * pt.k_s[1] + G * 16;
+    const char* vbase = pt.v + place.cache * pt.v_s[0] + place.g * pt.v_s[1] + n * (CW * ES);
     const uint32_t krow = (uint32_t)pt.k_s[2], vrow = (uint32_t)pt.v_s[2];
 
     u32x4 kf[2][KC];
@@ -233,7 +240,16 @@ __device__ __forceinline__ void prefix_keys(const PrefixArgs& a, int wg, char* s
         load_k(t);
         load_v(t);
     }
-    if constexpr (OWN) build_ancestors(tid, w.cache, a.T, w.Tq, a.parents, tree.par, tree.anc);
+    bool valid[RB];
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+        valid[rb] = prefix_row_exists<OWN>(a, w, row[rb], (place.rg * RB + rb) * 16 + n);
+        if (!valid[rb]) {
+#pragma unroll
+            for (int c = 0; c < KC; ++c) qf[rb][c] = u32x4{0, 0, 0, 0};
+        }
+    }
+    if constexpr (OWN) build_ancestors(tid, place.cache, a.T, w.Tq, a.parents, tree.par, tree.anc);
     for (; t < t1; t += kPrefixWaves) {
         const int next = t + kPrefixWaves;
         f32x4 s[RB][2];
@@ -329,8 +345,8 @@ __device__ __forceinline__ void prefix_keys(const PrefixArgs& a, int wg, char* s
         for (int o = 0; o < kPrefixWaves; ++o)
             if (!(s_z[o][rb * 16 + n] == 0.f)) Z += s_z[o][rb * 16 + n] * fast_exp2(s_m[o][rb * 16 + n] - M);
         const float f = z[rb] == 0.f ? 0.f : fast_exp2(mref[rb] * a.scale_log2 - M);
-        const int64_t slot = (int64_t)(pt.slot0 + w.slice) * a.rows_total;
-        if (wave == 0 && G == 0 && row[rb].valid)
+        const int64_t slot = (int64_t)(pt.slot0 + place.slice) * a.rows_total;
+        if (wave == 0 && G == 0 && valid[rb])
             *reinterpret_cast<float2*>(a.part_stats + (slot + prefix_state_row(a, row[rb])) * 2) = make_float2(M, Z);
         if (t0 >= t1) continue;                      // (uniform) an empty slice leaves Z = 0 and no sums
         if (rb > 0) __syncthreads();
@@ -346,8 +362,9 @@ __device__ __forceinline__ void prefix_keys(const PrefixArgs& a, int wg, char* s
             f32x4 sum = *reinterpret_cast<const f32x4*>(s_acc + rr * PITCH + c);
 #pragma unroll
             for (int o = 1; o < kPrefixWaves; ++o) sum += *reinterpret_cast<const f32x4*>(s_acc + (o * 16 + rr) * PITCH + c);
-            const PrefixRow x = prefix_row<OWN>(a, w, (w.rg * RB + rb) * 16 + rr);
-            if (x.valid) *reinterpret_cast<f32x4*>(a.part_acc + (slot + prefix_state_row(a, x)) * DV + c) = sum;
+            const int r = (place.rg * RB + rb) * 16 + rr;
+            const PrefixRow x = prefix_row<OWN>(a, place, r);
+            if (prefix_row_exists<OWN>(a, w, x, r)) *reinterpret_cast<f32x4*>(a.part_acc + (slot + prefix_state_row(a, x)) * DV + c) = sum;
         }
     }
 }
@@ -384,7 +401,20 @@ __device__ __forceinline__ void prefix_rows(const PrefixArgs& a, int wg, char* s
     const PrefixPart& pt = a.part[OWN];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n = lane & 31, hb = lane >> 5;
-    const PrefixWork w = prefix_work<OWN>(a, wg);
+
+    // ---- rows: B operands of S^T = K Q^T, row n of this wavefront's block, all contraction steps
+    const PrefixPlace place = prefix_place<OWN>(a, wg);
+    const int r0 = place.rg * Cfg::ROWS + wave * 32;
+    const bool live = r0 < pt.rows;                               // (uniform) the wavefront has rows
+    const PrefixRow row = prefix_row<OWN>(a, place, r0 + n);
+    u32x4 qf[STEPS];
+    {
+        const char* qp = a.q + row.b * a.q_s[0] + row.i * a.q_s[1] + row.h * a.q_s[2] + hb * 16;
+#pragma unroll
+        for (int st = 0; st < STEPS; ++st) qf[st] = *reinterpret_cast<const u32x4*>(qp + st * 32);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    const PrefixWork w = prefix_work<OWN>(a, place);
     const int t0 = w.t0, t1 = w.t1;
 
     // ---- tile loads: K(t), then V(t), in one of three stages of the ring that take turns.  A load moves its pointer on, so that
@@ -392,8 +422,8 @@ __device__ __forceinline__ void prefix_rows(const PrefixArgs& a, int wg, char* s
     //      an empty buffer, which fetch nothing (the counted waits below need no cases).
     const uint32_t krow = (uint32_t)pt.k_s[2], vrow = (uint32_t)pt.v_s[2];
     const int64_t kstep = pt.k_s[2] * kTile, vstep = pt.v_s[2] * kTile;
-    const char* knext = pt.k + w.cache * pt.k_s[0] + w.g * pt.k_s[1] + t0 * kstep;      // of the next tile to load
-    const char* vnext = pt.v + w.cache * pt.v_s[0] + w.g * pt.v_s[1] + t0 * vstep;
+    const char* knext = pt.k + place.cache * pt.k_s[0] + place.g * pt.k_s[1] + t0 * kstep;      // of the next tile to load
+    const char* vnext = pt.v + place.cache * pt.v_s[0] + place.g * pt.v_s[1] + t0 * vstep;
     int kleft = w.n_keys - t0 * kTile, vleft = kleft;             // rows from there on
     int kt_left = t1 - t0, vt_left = t1 - t0;                     // tiles of the slice from there on
     KLoader kld;
@@ -419,20 +449,11 @@ __device__ __forceinline__ void prefix_rows(const PrefixArgs& a, int wg, char* s
     auto load_v = [&] { load(vld, vnext, vstep, vrow, vleft, vt_left, vdst, vstage); };
     if (t0 < t1) load_k();
 
-    // ---- rows: B operands of S^T = K Q^T, row n of this wavefront's block, all contraction steps
-    const int r0 = w.rg * Cfg::ROWS + wave * 32;
-    const bool live = r0 < pt.rows;                               // (uniform) the wavefront has rows
-    const PrefixRow row = prefix_row<OWN>(a, w, r0 + n);
-    u32x4 qf[STEPS];
-    {
-        const char* qp = a.q + row.b * a.q_s[0] + row.i * a.q_s[1] + row.h * a.q_s[2] + hb * 16;
-#pragma unroll
-        for (int st = 0; st < STEPS; ++st) qf[st] = *reinterpret_cast<const u32x4*>(qp + st * 32);
-    }
-    if constexpr (OWN) build_ancestors(tid, w.cache, a.T, w.Tq, a.parents, tree.par, tree.anc);
+    const bool valid = prefix_row_exists<OWN>(a, w, row, r0 + n);
+    if constexpr (OWN) build_ancestors(tid, place.cache, a.T, w.Tq, a.parents, tree.par, tree.anc);
     const AncSet anc = OWN ? tree.anc[row.i] : AncSet{0ull, 0ull};
     arrived(qf);
-    if (!row.valid) {
+    if (!valid) {
 #pragma unroll
         for (int st = 0; st < STEPS; ++st) qf[st] = u32x4{0, 0, 0, 0};
     }
@@ -607,8 +628,8 @@ __device__ __forceinline__ void prefix_rows(const PrefixArgs& a, int wg, char* s
 
     // ---- partial state of this slice: (reference maximum, Z) per row and the un-normalised accumulator; lane layout of
     //      acc[mb]: row n of the block, columns 32 mb + 8 j + 4 hb + r at vector index 4 j + r
-    if (row.valid) {
-        const int64_t pr = (int64_t)(pt.slot0 + w.slice) * a.rows_total + prefix_state_row(a, row);
+    if (valid) {
+        const int64_t pr = (int64_t)(pt.slot0 + place.slice) * a.rows_total + prefix_state_row(a, row);
         if (hb == 0) *reinterpret_cast<float2*>(a.part_stats + pr * 2) = make_float2(mref * a.scale_log2, zrun);
         if (!(zrun == 0.f)) {
 #pragma unroll
@@ -634,6 +655,7 @@ template <bool BF16, int DK, int DV, int PREFIX, int OWN>
 __global__ void __launch_bounds__(kPrefixThreads, 1) __attribute__((amdgpu_waves_per_eu(2, 2))) k_prefix(const PrefixArgs a) {
     extern __shared__ __align__(16) char smem[];
     __shared__ PrefixTree tree;
+    touch_args<PrefixArgs>();
     const int n0 = a.part[0].n_pad;
     if ((int)blockIdx.x < n0) {
         const int wg = (blockIdx.x & 7) * (n0 >> 3) + (blockIdx.x >> 3);

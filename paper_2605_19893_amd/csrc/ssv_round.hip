@@ -46,34 +46,38 @@ int plan_rows(PartPlan* pt, bool bf16, int H_kv) {
     return (int64_t)pt->caches * H_kv * pt->n_rg * kPrefixMaxSlices > (1 << 24) ? SSV_EUNSUPPORTED : SSV_OK;
 }
 
-// What a part would cost in n slices: workgroups, and microseconds of one.  A rough model, measured at full load: a tile takes a
-// workgroup of the rows path 52 ns per matrix instruction of a wavefront (with at most four wavefronts, one per SIMD, two thirds
-// of it), one of the keys path its bytes at 80 GB/s (fp32: its products); every workgroup 7 us from its first instruction to its first tile and
-// from its last one to its end.
-struct SliceCost { int n, wgs; float us; };
+// What a part would cost in n slices: workgroups, and microseconds of the longest and of an average one.  A rough model from in-kernel
+// clocks: a tile takes a workgroup of the rows path 2.1 us at 192 + 128 and 1.1 us at 64 + 64 (with at most one wavefront per SIMD
+// 1.1 and 0.8), one of the keys path what its bytes take at 60 GB/s; 7 us pass from the first instruction to the first tile and
+// from the last one to the end.
+struct SliceCost { int n, wgs; float us, mean; };
 struct PartCost {
-    float tile_us;
+    float tile_us, mean;
     int tiles, groups;
-    PartCost(const PartPlan& pt, const ssv_prefix_params* p, int64_t max_keys, float share) {
-        const float mma = (p->d_k + p->d_v) / 8.f, bytes = 64.f * (p->d_k + p->d_v) * (p->dtype == SSV_BF16 ? 2 : 4);
-        tile_us = share * (pt.path == 0 ? 0.052f * mma * (pt.rows > 128 ? 1.f : 0.67f) : (p->dtype == SSV_BF16 ? bytes / 80e3f : pt.path * 0.9f));
+    PartCost(const PartPlan& pt, const ssv_prefix_params* p, int64_t max_keys, float mean_share) : mean(mean_share) {
+        const float mma = (p->d_k + p->d_v) / 8.f, bytes = 64.f * (p->d_k + p->d_v) * 2;
+        tile_us = p->dtype == SSV_F32 ? 0.6f * pt.path
+                  : pt.path            ? bytes / 60e3f
+                                       : (pt.rows > 128 ? 0.35f + 0.044f * mma : 0.6f + 0.0135f * mma);
         tiles = (int)((max_keys + kTile - 1) / kTile);
         groups = pt.caches * p->H_kv * pt.n_rg;
     }
     SliceCost at(int n) const {
-        const int chunk = std::max(kPrefixMinTiles, (tiles + n - 1) / n);
-        return SliceCost{(tiles + chunk - 1) / chunk, groups * ((tiles + chunk - 1) / chunk), 7.f + chunk * tile_us};
+        const int chunk = std::max(kPrefixMinTiles, (tiles + n - 1) / n), slices = (tiles + chunk - 1) / chunk;
+        return SliceCost{slices, groups * slices, 7.f + chunk * tile_us, 7.f + chunk * tile_us * mean};
     }
 };
+// n workgroups of mixed lengths on `cus` compute units, in any order
+float spread_us(const SliceCost& c, float n, float cus) { return n <= 0 ? 0.f : n <= cus ? c.us : n * c.mean / cus + c.us / 2; }
 
 // Slices of both parts: the pair with the least estimated time for one launch (the prefix's workgroups in rounds of 256, the own
 // ones in the places they leave) and for the partial states, which are written and read back at 4 TB/s.
 void plan_slices(PrefixLayout* lo, const ssv_prefix_params* p) {
-    static constexpr int counts[] = {1, 2, 3, 4, 5, 6, 7, 8, 10, 12, 14, 16, 20, 24, 28, 32};
+    static constexpr int counts[] = {1, 2, 3, 4, 5, 6, 7, 8, 9, 10, 12, 14, 16, 18, 20, 24, 28, 32, 40, 48, 64};
     constexpr int N = sizeof(counts) / sizeof(counts[0]);
     const bool shared = p->max_prefix_len > 0;
-    SliceCost own[N], first = {0, 0, 0.f};
-    const PartCost oc(lo->part[1], p, (int64_t)p->max_seq_len + p->T, 0.75f);       // (sequences of mixed lengths, the bound is the longest's)
+    SliceCost own[N], first = {0, 0, 0.f, 0.f};
+    const PartCost oc(lo->part[1], p, (int64_t)p->max_seq_len + p->T, 0.5f);       // (sequences of mixed lengths, the bound is the longest's)
     int n_own = 0;
     for (int n : counts) {
         const SliceCost c = oc.at(n);
@@ -86,16 +90,12 @@ void plan_slices(PrefixLayout* lo, const ssv_prefix_params* p) {
         if (shared) first = PartCost(lo->part[0], p, p->max_prefix_len, 1.f).at(counts[i]);
         if (first.n == last) continue;
         last = first.n;
-        const int full = first.wgs / kPrefixWgs, rest = first.wgs % kPrefixWgs, idle = kPrefixWgs - rest;
+        const int full = first.wgs / kPrefixWgs, rest = first.wgs % kPrefixWgs;
+        const float idle = rest ? kPrefixWgs - rest : 0, done = (full + (rest ? 1 : 0)) * first.us;
         for (int j = 0; j < n_own; ++j) {
             const SliceCost& c = own[j];
-            const float done = (full + (rest ? 1 : 0)) * first.us;
-            // the own workgroups fit beside the last round, or wait for it, or use its idle places alone
-            const int beside = rest ? idle * (int)(first.us / c.us) : 0;
-            float us = done;
-            if (c.wgs > beside)
-                us = std::min(done + (c.wgs - beside + kPrefixWgs - 1) / kPrefixWgs * c.us,
-                              std::max(done, full * first.us + (c.wgs + idle - 1) / idle * c.us));
+            float us = done + spread_us(c, c.wgs, kPrefixWgs);       // behind the prefix's workgroups, or in the idle places of their last round
+            if (idle > 0) us = std::min(us, std::max(done, full * first.us + spread_us(c, c.wgs, idle)));
             us += (first.n + c.n) * slot_us;
             if (us < best) {
                 best = us;
@@ -202,6 +202,7 @@ int prefix_launch(const void* q, const void* kp, const void* vp, const void* k, 
     a.rows_total = lo.rows_total;
     a.div_TH = FastDiv::of(p->T * lo.H_g);
     a.div_Hg = FastDiv::of(lo.H_g);
+    a.div_Hkv = FastDiv::of(p->H_kv);
     for (int j = 0; j < 3; ++j) a.q_s[j] = lo.q_s[j];
     for (int own = 0; own < 2; ++own) {
         const PartPlan& pl = lo.part[own];
@@ -212,6 +213,8 @@ int prefix_launch(const void* q, const void* kp, const void* vp, const void* k, 
         pt.per = pl.per; pt.rows = pl.rows; pt.n_rg = pl.n_rg;
         pt.max_len = own ? p->max_seq_len : p->max_prefix_len;
         pt.n_slices = pl.n_slices;
+        pt.div_rg = FastDiv::of(pl.n_rg);
+        pt.div_slices = FastDiv::of(pl.n_slices);
         pt.slot0 = own ? lo.part[0].n_slices : 0;
         pt.n_wg = pl.n_wg;
         pt.n_pad = (int)align_up(pl.n_wg, 8);
