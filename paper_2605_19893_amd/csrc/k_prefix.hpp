@@ -15,17 +15,21 @@
 #include <type_traits>
 
 #include "device_common.hpp"
+#include "wave_ops.hpp"
 
 namespace ssv {
 
 struct PrefixPart {
     const char *k, *v;                 // the prefixes, or the sequences' own caches
     const int32_t* lens;               // rows of each prefix, or committed tokens of each sequence
-    int per;                           // sequences that share a cache (1: the sequences' own)
+    int caches, per;                   // per: sequences that share a cache (1: the sequences' own)
     int rows, n_rg;                    // rows per (cache, KV head); groups of them, one per workgroup
     int max_len;
-    int n_slices, slot0;               // slices per pair, and the first one's partial-state slot
-    FastDiv div_rg, div_slices;
+    int units;                         // slices of all caches together; each is taken by H_kv * n_rg workgroups
+    int slots, slot0;                  // partial-state slots per row (slices a cache can have), and the first one
+    int min_tiles;                     // tiles of 64 keys that a slice holds at least
+    int by_length;                     // 1: the slices are dealt out by the lengths; 0: units / caches to every cache
+    FastDiv div_groups, div_rg, div_slices;
     int n_wg, n_pad;                   // workgroups, and the same rounded up to a multiple of 8
     int64_t k_s[3], v_s[3];            // bytes: cache, KV head, row
 };
@@ -38,7 +42,7 @@ struct PrefixArgs {
     int T, H, H_kv, H_g;
     float scale_log2;
     int64_t rows_total;
-    FastDiv div_TH, div_Hg, div_Hkv;
+    FastDiv div_TH, div_Hg;
     int64_t q_s[3];                    // bytes: sequence, node, head
 };
 
@@ -47,6 +51,7 @@ constexpr int kPrefixWaves = kPrefixThreads / 64;
 constexpr int kPrefixStep = 32;        // keys per step of a wavefront on the keys path
 constexpr int kPrefixMaxSlots = 128;   // partial states per row
 constexpr int kPrefixMinTiles = 2;     // tiles of 64 keys that a slice holds at least
+constexpr int kPrefixMaxDealt = 64;    // caches whose slices are dealt out by length: a lane each
 constexpr float kPrefixRaiseLog2 = 8.f;   // the reference maximum follows the running one at a distance of up to 2^8
 
 struct PrefixTree {                    // LDS: the draft tree of one sequence
@@ -94,49 +99,76 @@ __device__ __forceinline__ float add_bf16_pair(uint32_t pair, float sum) {
     return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pair), __builtin_bit_cast(bf16x2, 0x3f803f80u), sum, false);
 }
 
-// What a workgroup of either path works on: its place in the launch, and what the lengths make of it.  The place gives the
-// addresses of the queries, which are fetched while the lengths are on their way.
-struct PrefixPlace { int rg, slice, cache, g; };
-template <bool OWN>
-__device__ __forceinline__ PrefixPlace prefix_place(const PrefixArgs& a, int wg) {
-    const PrefixPart& pt = a.part[OWN];
-    PrefixPlace w;
-    const int ps = pt.div_rg.div(wg);                      // neighbours read the same keys
-    w.rg = wg - ps * pt.n_rg;
-    const int pair = pt.div_slices.div(ps);
-    w.slice = ps - pair * pt.n_slices;
-    w.cache = a.div_Hkv.div(pair);
-    w.g = pair - w.cache * a.H_kv;
-    return w;
-}
+// What a workgroup of either path works on.
+//
+// The host deals out workgroups without knowing the lengths.  With up to 64 caches every wavefront reads them all, a lane each,
+// and finds the least slice length L (nearly) for which the slices of all caches are no more than the units there are:
+//   sum_c max(1, ceil(tiles_c / L)) <= units;
+// slices are then equally long whatever the lengths are.  (Two prompts of 12K and 6K rows with equal counts: the shorter one's
+// workgroups are done in half the time.)  With one cache, or more than 64, every cache has the same number of slices.
 struct PrefixWork {
+    int rg, slice, cache, g;
     int len, Tq, n_keys;               // Tq: nodes of the sequence (own caches only)
     int t0, t1;                        // tiles of 64 keys
+    bool any, last;                    // there is a slice for this workgroup; it is its cache's last one
 };
 template <bool OWN>
-__device__ __forceinline__ PrefixWork prefix_work(const PrefixArgs& a, const PrefixPlace& at) {
+__device__ __forceinline__ PrefixWork prefix_work(const PrefixArgs& a, int wg) {
     const PrefixPart& pt = a.part[OWN];
     PrefixWork w;
-    w.len = min(max(pt.lens[at.cache], 0), pt.max_len);
-    w.Tq = OWN ? (a.n_query ? min(max(a.n_query[at.cache], 0), a.T) : a.T) : 0;
-    w.n_keys = w.len + w.Tq;
-    const int n_tiles = (w.n_keys + kTile - 1) / kTile;
-    const int chunk = max(pt.div_slices.div(n_tiles + pt.n_slices - 1), kPrefixMinTiles);
-    w.t0 = min(n_tiles, at.slice * chunk);
-    w.t1 = min(n_tiles, w.t0 + chunk);
+    const int unit = pt.div_groups.div(wg), in = wg - unit * (a.H_kv * pt.n_rg);
+    w.g = pt.div_rg.div(in);
+    w.rg = in - w.g * pt.n_rg;                             // neighbours read the same keys
+    if (pt.by_length) {                                    // (uniform)
+        const int c = threadIdx.x & 63, cc = min(c, pt.caches - 1);
+        const int len = min(max(pt.lens[cc], 0), pt.max_len);
+        const int Tq = OWN ? (a.n_query ? min(max(a.n_query[cc], 0), a.T) : a.T) : 0;
+        const bool there = c < pt.caches && (!OWN || Tq > 0);      // (a sequence without nodes has no rows)
+        const int tiles = there ? (len + Tq + kTile - 1) / kTile : 0;
+        int L = max(pt.min_tiles, (wave_sum(tiles) + pt.units - 1) / pt.units), n, end;
+        for (;;) {                     // ends: with L at the longest cache's tiles there is one slice per cache
+            n = there ? max(1, (tiles + L - 1) / L) : 0;
+            end = wave_incl_scan(n);
+            if (last_lane(end) <= pt.units) break;
+            L += max(1, L >> 4);
+        }
+        const uint64_t m = __builtin_amdgcn_ballot_w64(n > 0 && end - n <= unit);
+        w.any = unit < last_lane(end);
+        w.cache = m ? 63 - __builtin_clzll(m) : 0;
+        w.slice = unit - __builtin_amdgcn_readlane(end - n, w.cache);
+        w.last = w.slice + 1 == __builtin_amdgcn_readlane(n, w.cache);
+        w.len = __builtin_amdgcn_readlane(len, w.cache);
+        w.Tq = __builtin_amdgcn_readlane(Tq, w.cache);
+        w.n_keys = w.len + w.Tq;
+        const int n_tiles = (w.n_keys + kTile - 1) / kTile;
+        w.t0 = min(n_tiles, w.slice * L);
+        w.t1 = min(n_tiles, w.t0 + L);
+    } else {
+        w.cache = pt.div_slices.div(unit);
+        w.slice = unit - w.cache * pt.slots;
+        w.any = true;
+        w.last = w.slice + 1 == pt.slots;
+        w.len = min(max(pt.lens[w.cache], 0), pt.max_len);
+        w.Tq = OWN ? (a.n_query ? min(max(a.n_query[w.cache], 0), a.T) : a.T) : 0;
+        w.n_keys = w.len + w.Tq;
+        const int n_tiles = (w.n_keys + kTile - 1) / kTile;
+        const int L = max(pt.div_slices.div(n_tiles + pt.slots - 1), pt.min_tiles);
+        w.t0 = min(n_tiles, w.slice * L);
+        w.t1 = min(n_tiles, w.t0 + L);
+    }
     return w;
 }
 
 // Row r of a (cache, KV head): its sequence, node and head; and whether it exists.
 struct PrefixRow { int b, i, h; };
 template <bool OWN>
-__device__ __forceinline__ PrefixRow prefix_row(const PrefixArgs& a, const PrefixPlace& at, int r) {
+__device__ __forceinline__ PrefixRow prefix_row(const PrefixArgs& a, const PrefixWork& w, int r) {
     const int rc = min(r, a.part[OWN].rows - 1);
     const int bl = OWN ? 0 : a.div_TH.div(rc), in = rc - bl * a.T * a.H_g;
     PrefixRow x;
     x.i = a.div_Hg.div(in);
-    x.h = at.g * a.H_g + in - x.i * a.H_g;
-    x.b = at.cache * a.part[OWN].per + bl;
+    x.h = w.g * a.H_g + in - x.i * a.H_g;
+    x.b = w.cache * a.part[OWN].per + bl;
     return x;
 }
 template <bool OWN>
@@ -144,6 +176,14 @@ __device__ __forceinline__ bool prefix_row_exists(const PrefixArgs& a, const Pre
     return r < a.part[OWN].rows && x.i < (OWN ? w.Tq : (a.n_query ? a.n_query[x.b] : a.T));
 }
 __device__ __forceinline__ int64_t prefix_state_row(const PrefixArgs& a, const PrefixRow& x) { return ((int64_t)x.b * a.T + x.i) * a.H + x.h; }
+
+// (m, Z) of a row's slice; the cache's last slice marks the slots behind its own as empty.
+__device__ __forceinline__ void put_statistics(const PrefixArgs& a, const PrefixPart& pt, const PrefixWork& w, int64_t row, float m, float Z) {
+    float* at = a.part_stats + ((int64_t)(pt.slot0 + w.slice) * a.rows_total + row) * 2;
+    *reinterpret_cast<float2*>(at) = make_float2(m, Z);
+    if (w.last)
+        for (int s = w.slice + 1; s < pt.slots; ++s) *reinterpret_cast<float2*>(at += a.rows_total * 2) = make_float2(0.f, 0.f);
+}
 
 // ---- keys path --------------------------------------------------------------------------------------------------------
 // One workgroup = 16 RB rows of one (cache, KV head) x one slice of its keys.  Its wavefronts hold the same rows and take
@@ -172,23 +212,22 @@ __device__ __forceinline__ void prefix_keys(const PrefixArgs& a, int wg, char* s
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int n = lane & 15, G = lane >> 4;
     // ---- rows
-    const PrefixPlace place = prefix_place<OWN>(a, wg);
+    const PrefixWork w = prefix_work<OWN>(a, wg);
+    if (!w.any) return;
     PrefixRow row[RB];
     u32x4 qf[RB][KC];
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
-        row[rb] = prefix_row<OWN>(a, place, (place.rg * RB + rb) * 16 + n);
+        row[rb] = prefix_row<OWN>(a, w, (w.rg * RB + rb) * 16 + n);
         const char* qp = a.q + row[rb].b * a.q_s[0] + row[rb].i * a.q_s[1] + row[rb].h * a.q_s[2] + G * 16;
 #pragma unroll
         for (int c = 0; c < KC; ++c) qf[rb][c] = *reinterpret_cast<const u32x4*>(qp + c * 64);
     }
-    __builtin_amdgcn_sched_barrier(0);
-    const PrefixWork w = prefix_work<OWN>(a, place);
 
     // ---- this slice's steps
     const int t0 = w.t0 * (kTile / kPrefixStep), t1 = min(w.t1 * (kTile / kPrefixStep), (w.n_keys + kPrefixStep - 1) / kPrefixStep);
-    const char* kbase = pt.k + place.cache * pt.k_s[0] + place.g * pt.k_s[1] + G * 16;
-    const char* vbase = pt.v + place.cache * pt.v_s[0] + place.g * pt.v_s[1] + n * (CW * ES);
+    const char* kbase = pt.k + w.cache * pt.k_s[0] + w.g * pt.k_s[1] + G * 16;
+    const char* vbase = pt.v + w.cache * pt.v_s[0] + w.g * pt.v_s[1] + n * (CW * ES);
     const uint32_t krow = (uint32_t)pt.k_s[2], vrow = (uint32_t)pt.v_s[2];
 
     u32x4 kf[2][KC];
@@ -243,13 +282,13 @@ __device__ __forceinline__ void prefix_keys(const PrefixArgs& a, int wg, char* s
     bool valid[RB];
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
-        valid[rb] = prefix_row_exists<OWN>(a, w, row[rb], (place.rg * RB + rb) * 16 + n);
+        valid[rb] = prefix_row_exists<OWN>(a, w, row[rb], (w.rg * RB + rb) * 16 + n);
         if (!valid[rb]) {
 #pragma unroll
             for (int c = 0; c < KC; ++c) qf[rb][c] = u32x4{0, 0, 0, 0};
         }
     }
-    if constexpr (OWN) build_ancestors(tid, place.cache, a.T, w.Tq, a.parents, tree.par, tree.anc);
+    if constexpr (OWN) build_ancestors(tid, w.cache, a.T, w.Tq, a.parents, tree.par, tree.anc);
     for (; t < t1; t += kPrefixWaves) {
         const int next = t + kPrefixWaves;
         f32x4 s[RB][2];
@@ -345,9 +384,8 @@ __device__ __forceinline__ void prefix_keys(const PrefixArgs& a, int wg, char* s
         for (int o = 0; o < kPrefixWaves; ++o)
             if (!(s_z[o][rb * 16 + n] == 0.f)) Z += s_z[o][rb * 16 + n] * fast_exp2(s_m[o][rb * 16 + n] - M);
         const float f = z[rb] == 0.f ? 0.f : fast_exp2(mref[rb] * a.scale_log2 - M);
-        const int64_t slot = (int64_t)(pt.slot0 + place.slice) * a.rows_total;
-        if (wave == 0 && G == 0 && valid[rb])
-            *reinterpret_cast<float2*>(a.part_stats + (slot + prefix_state_row(a, row[rb])) * 2) = make_float2(M, Z);
+        const int64_t slot = (int64_t)(pt.slot0 + w.slice) * a.rows_total;
+        if (wave == 0 && G == 0 && valid[rb]) put_statistics(a, pt, w, prefix_state_row(a, row[rb]), M, Z);
         if (t0 >= t1) continue;                      // (uniform) an empty slice leaves Z = 0 and no sums
         if (rb > 0) __syncthreads();
 #pragma unroll
@@ -362,8 +400,8 @@ __device__ __forceinline__ void prefix_keys(const PrefixArgs& a, int wg, char* s
             f32x4 sum = *reinterpret_cast<const f32x4*>(s_acc + rr * PITCH + c);
 #pragma unroll
             for (int o = 1; o < kPrefixWaves; ++o) sum += *reinterpret_cast<const f32x4*>(s_acc + (o * 16 + rr) * PITCH + c);
-            const int r = (place.rg * RB + rb) * 16 + rr;
-            const PrefixRow x = prefix_row<OWN>(a, place, r);
+            const int r = (w.rg * RB + rb) * 16 + rr;
+            const PrefixRow x = prefix_row<OWN>(a, w, r);
             if (prefix_row_exists<OWN>(a, w, x, r)) *reinterpret_cast<f32x4*>(a.part_acc + (slot + prefix_state_row(a, x)) * DV + c) = sum;
         }
     }
@@ -403,27 +441,26 @@ __device__ __forceinline__ void prefix_rows(const PrefixArgs& a, int wg, char* s
     const int n = lane & 31, hb = lane >> 5;
 
     // ---- rows: B operands of S^T = K Q^T, row n of this wavefront's block, all contraction steps
-    const PrefixPlace place = prefix_place<OWN>(a, wg);
-    const int r0 = place.rg * Cfg::ROWS + wave * 32;
+    const PrefixWork w = prefix_work<OWN>(a, wg);
+    if (!w.any) return;
+    const int t0 = w.t0, t1 = w.t1;
+    const int r0 = w.rg * Cfg::ROWS + wave * 32;
     const bool live = r0 < pt.rows;                               // (uniform) the wavefront has rows
-    const PrefixRow row = prefix_row<OWN>(a, place, r0 + n);
+    const PrefixRow row = prefix_row<OWN>(a, w, r0 + n);
     u32x4 qf[STEPS];
     {
         const char* qp = a.q + row.b * a.q_s[0] + row.i * a.q_s[1] + row.h * a.q_s[2] + hb * 16;
 #pragma unroll
         for (int st = 0; st < STEPS; ++st) qf[st] = *reinterpret_cast<const u32x4*>(qp + st * 32);
     }
-    __builtin_amdgcn_sched_barrier(0);
-    const PrefixWork w = prefix_work<OWN>(a, place);
-    const int t0 = w.t0, t1 = w.t1;
 
     // ---- tile loads: K(t), then V(t), in one of three stages of the ring that take turns.  A load moves its pointer on, so that
     //      offsets stay within a tile however long the cache is; past the slice's last tile it is the same instructions with
     //      an empty buffer, which fetch nothing (the counted waits below need no cases).
     const uint32_t krow = (uint32_t)pt.k_s[2], vrow = (uint32_t)pt.v_s[2];
     const int64_t kstep = pt.k_s[2] * kTile, vstep = pt.v_s[2] * kTile;
-    const char* knext = pt.k + place.cache * pt.k_s[0] + place.g * pt.k_s[1] + t0 * kstep;      // of the next tile to load
-    const char* vnext = pt.v + place.cache * pt.v_s[0] + place.g * pt.v_s[1] + t0 * vstep;
+    const char* knext = pt.k + w.cache * pt.k_s[0] + w.g * pt.k_s[1] + t0 * kstep;      // of the next tile to load
+    const char* vnext = pt.v + w.cache * pt.v_s[0] + w.g * pt.v_s[1] + t0 * vstep;
     int kleft = w.n_keys - t0 * kTile, vleft = kleft;             // rows from there on
     int kt_left = t1 - t0, vt_left = t1 - t0;                     // tiles of the slice from there on
     KLoader kld;
@@ -450,7 +487,7 @@ __device__ __forceinline__ void prefix_rows(const PrefixArgs& a, int wg, char* s
     if (t0 < t1) load_k();
 
     const bool valid = prefix_row_exists<OWN>(a, w, row, r0 + n);
-    if constexpr (OWN) build_ancestors(tid, place.cache, a.T, w.Tq, a.parents, tree.par, tree.anc);
+    if constexpr (OWN) build_ancestors(tid, w.cache, a.T, w.Tq, a.parents, tree.par, tree.anc);
     const AncSet anc = OWN ? tree.anc[row.i] : AncSet{0ull, 0ull};
     arrived(qf);
     if (!valid) {
@@ -629,8 +666,8 @@ __device__ __forceinline__ void prefix_rows(const PrefixArgs& a, int wg, char* s
     // ---- partial state of this slice: (reference maximum, Z) per row and the un-normalised accumulator; lane layout of
     //      acc[mb]: row n of the block, columns 32 mb + 8 j + 4 hb + r at vector index 4 j + r
     if (valid) {
-        const int64_t pr = (int64_t)(pt.slot0 + place.slice) * a.rows_total + prefix_state_row(a, row);
-        if (hb == 0) *reinterpret_cast<float2*>(a.part_stats + pr * 2) = make_float2(mref * a.scale_log2, zrun);
+        const int64_t pr = (int64_t)(pt.slot0 + w.slice) * a.rows_total + prefix_state_row(a, row);
+        if (hb == 0) put_statistics(a, pt, w, prefix_state_row(a, row), mref * a.scale_log2, zrun);
         if (!(zrun == 0.f)) {
 #pragma unroll
             for (int mb = 0; mb < MB; ++mb)
@@ -717,17 +754,17 @@ __global__ void __launch_bounds__(kThreads) k_prefix_combine(const PrefixCombine
 #pragma unroll
     for (int k = 0; k < PER; ++k)
         for (int s0 = k * TPR; s0 < (k + 1) * TPR && s0 < a.n_slots; s0 += BATCH) {
-            if (s0) {
-#pragma unroll
-                for (int s = 0; s < BATCH; ++s) v[s] = *reinterpret_cast<const f32x4*>(at + min(s0 + s, a.n_slots - 1) * step);
-            }
+            // slots that saw no key, or that do not exist, hold anything: their weight is 0, and from the second batch on they are not fetched
+            float ws[BATCH];
 #pragma unroll
             for (int s = 0; s < BATCH; ++s) {
-                // (slots that saw no key, or that do not exist, hold anything: their weight is 0)
-                const float ws = __shfl(w[k], s0 - k * TPR + s, TPR);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) acc[e] += ws == 0.f ? 0.f : ws * v[s][e];
+                ws[s] = __shfl(w[k], s0 - k * TPR + s, TPR);
+                if (s0 && ws[s] != 0.f) v[s] = *reinterpret_cast<const f32x4*>(at + (s0 + s) * step);
             }
+#pragma unroll
+            for (int s = 0; s < BATCH; ++s)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[e] += ws[s] == 0.f ? 0.f : ws[s] * v[s][e];
         }
     acc *= 1.f / Z;
     if (i >= Tq) acc = f32x4{0.f, 0.f, 0.f, 0.f};       // (a node that exists sees itself: Z > 0)

@@ -27,12 +27,14 @@ constexpr int kPrefixMaxSlices = kPrefixMaxSlots / 2;      // per part (prefix, 
 constexpr int kPrefixWgs = 256;            // one round of workgroups: one per CU
 
 struct PartPlan {
-    int caches, per, rows, path, n_rg, n_slices, n_wg;
+    int caches, per, rows, path, n_rg;
+    int units, slots, min_tiles;       // slices of all caches together (0: no such part), slots per row, tiles per slice at least
+    bool by_length;
 };
 
 struct PrefixLayout {
     int H_g, es;
-    PartPlan part[2];            // prefix (n_slices = 0: none), own rows
+    PartPlan part[2];            // prefix, own rows
     int n_slots;
     int64_t rows_total;
     int64_t q_s[3], out_s[3];    // bytes
@@ -41,30 +43,50 @@ struct PrefixLayout {
 
 // Path and row groups of a part.
 int plan_rows(PartPlan* pt, bool bf16, int H_kv) {
+    pt->by_length = pt->caches > 1 && pt->caches <= kPrefixMaxDealt;
     pt->path = pt->rows <= 16 ? 1 : (bf16 ? 0 : 2);
     pt->n_rg = ceil_div(pt->rows, pt->path ? 16 * pt->path : 256);
     return (int64_t)pt->caches * H_kv * pt->n_rg * kPrefixMaxSlices > (1 << 24) ? SSV_EUNSUPPORTED : SSV_OK;
 }
 
-// What a part would cost in n slices: workgroups, and microseconds of the longest and of an average one.  A rough model from in-kernel
-// clocks: a tile takes a workgroup of the rows path 2.1 us at 192 + 128 and 1.1 us at 64 + 64 (with at most one wavefront per SIMD
-// 1.1 and 0.8), one of the keys path what its bytes take at 60 GB/s; 7 us pass from the first instruction to the first tile and
-// from the last one to the end.
-struct SliceCost { int n, wgs; float us, mean; };
+// What a part would cost in a number of slices: workgroups, and microseconds of the longest and of an average one.  A rough model
+// from in-kernel clocks: a tile takes a workgroup of the rows path 2.1 us at 192 + 128 and 1.1 us at 64 + 64 (with at most one
+// wavefront per SIMD 1.1 and 0.8), one of the keys path what its bytes take at 60 GB/s; 7 us pass from the first instruction to the
+// first tile and from the last one to the end.
+struct SliceCost { int units, slots, min_tiles, wgs; float us, mean; };
 struct PartCost {
     float tile_us, mean;
-    int tiles, groups;
-    PartCost(const PartPlan& pt, const ssv_prefix_params* p, int64_t max_keys, float mean_share) : mean(mean_share) {
+    int tiles, groups, caches;
+    bool by_length;
+    PartCost(const PartPlan& pt, const ssv_prefix_params* p, int64_t max_keys, float mean_share) : mean(mean_share), caches(pt.caches), by_length(pt.by_length) {
         const float mma = (p->d_k + p->d_v) / 8.f, bytes = 64.f * (p->d_k + p->d_v) * 2;
         tile_us = p->dtype == SSV_F32 ? 0.6f * pt.path
                   : pt.path            ? bytes / 60e3f
                                        : (pt.rows > 128 ? 0.35f + 0.044f * mma : 0.6f + 0.0135f * mma);
         tiles = (int)((max_keys + kTile - 1) / kTile);
-        groups = pt.caches * p->H_kv * pt.n_rg;
+        groups = p->H_kv * pt.n_rg;
     }
-    SliceCost at(int n) const {
-        const int chunk = std::max(kPrefixMinTiles, (tiles + n - 1) / n), slices = (tiles + chunk - 1) / chunk;
-        return SliceCost{slices, groups * slices, 7.f + chunk * tile_us, 7.f + chunk * tile_us * mean};
+    // slices per cache in eighths (8 and more)
+    SliceCost at(int eighths) const {
+        SliceCost c;
+        if (by_length) {
+            c.units = caches * eighths / 8;
+            c.slots = std::min(kPrefixMaxSlices, 2 * ((eighths + 7) / 8) + 1);
+            c.min_tiles = std::max(kPrefixMinTiles, (tiles + c.slots - 1) / c.slots);
+            // lengths of which the slices are cut: the mean of the caches; a cache's last slice is half empty
+            const float all = tiles * mean * caches, longest = std::max((float)c.min_tiles, all / std::max(1.f, c.units - (mean < 1.f ? 0.5f * caches : 0.f)));
+            c.us = 7.f + std::min((float)tiles, longest) * tile_us;
+            c.mean = 7.f + all / c.units * tile_us;
+        } else {
+            const int chunk = std::max(kPrefixMinTiles, (tiles + eighths / 8 - 1) / (eighths / 8));
+            c.slots = (tiles + chunk - 1) / chunk;
+            c.units = caches * c.slots;
+            c.min_tiles = kPrefixMinTiles;
+            c.us = 7.f + chunk * tile_us;
+            c.mean = 7.f + chunk * tile_us * mean;
+        }
+        c.wgs = groups * c.units;
+        return c;
     }
 };
 // n workgroups of mixed lengths on `cus` compute units, in any order
@@ -73,36 +95,39 @@ float spread_us(const SliceCost& c, float n, float cus) { return n <= 0 ? 0.f : 
 // Slices of both parts: the pair with the least estimated time for one launch (the prefix's workgroups in rounds of 256, the own
 // ones in the places they leave) and for the partial states, which are written and read back at 4 TB/s.
 void plan_slices(PrefixLayout* lo, const ssv_prefix_params* p) {
-    static constexpr int counts[] = {1, 2, 3, 4, 5, 6, 7, 8, 9, 10, 12, 14, 16, 18, 20, 24, 28, 32, 40, 48, 64};
-    constexpr int N = sizeof(counts) / sizeof(counts[0]);
+    static constexpr int eighths[] = {8, 10, 12, 16, 20, 24, 32, 40, 48, 56, 64, 72, 80, 96, 112, 128, 144, 160, 192, 224, 256, 320, 384, 512};
+    constexpr int N = sizeof(eighths) / sizeof(eighths[0]);
     const bool shared = p->max_prefix_len > 0;
-    SliceCost own[N], first = {0, 0, 0.f, 0.f};
-    const PartCost oc(lo->part[1], p, (int64_t)p->max_seq_len + p->T, 0.5f);       // (sequences of mixed lengths, the bound is the longest's)
+    SliceCost own[N], first = {0, 0, 0, 0, 0.f, 0.f};
+    const PartCost oc(lo->part[1], p, (int64_t)p->max_seq_len + p->T, p->B > 1 ? 0.5f : 1.f);       // (sequences of mixed lengths, the bound is the longest's)
     int n_own = 0;
-    for (int n : counts) {
+    for (int n : eighths) {
         const SliceCost c = oc.at(n);
-        if (!n_own || c.n != own[n_own - 1].n) own[n_own++] = c;
+        if (!n_own || c.units > own[n_own - 1].units) own[n_own++] = c;
     }
-    const float slot_us = (float)lo->rows_total * (p->d_v * 4 + 8) * 2 / 4e6f;
+    const float state_us = (float)(p->d_v * 4 + 8) * 2 / 4e6f;       // of a partial state
+    auto put = [](PartPlan* pt, const SliceCost& c) {
+        pt->units = c.units;
+        pt->slots = c.slots;
+        pt->min_tiles = c.min_tiles;
+    };
     float best = 1e30f;
     int last = -1;
     for (int i = 0; i < (shared ? N : 1); ++i) {
-        if (shared) first = PartCost(lo->part[0], p, p->max_prefix_len, 1.f).at(counts[i]);
-        if (first.n == last) continue;
-        last = first.n;
+        if (shared) first = PartCost(lo->part[0], p, p->max_prefix_len, 1.f).at(eighths[i]);
+        if (first.units == last) continue;
+        last = first.units;
         const int full = first.wgs / kPrefixWgs, rest = first.wgs % kPrefixWgs;
         const float idle = rest ? kPrefixWgs - rest : 0, done = (full + (rest ? 1 : 0)) * first.us;
         for (int j = 0; j < n_own; ++j) {
             const SliceCost& c = own[j];
             float us = done + spread_us(c, c.wgs, kPrefixWgs);       // behind the prefix's workgroups, or in the idle places of their last round
             if (idle > 0) us = std::min(us, std::max(done, full * first.us + spread_us(c, c.wgs, idle)));
-            us += (first.n + c.n) * slot_us;
+            us += ((float)first.units * lo->part[0].rows + (float)c.units * lo->part[1].rows) * p->H_kv * state_us;
             if (us < best) {
                 best = us;
-                lo->part[0].n_slices = first.n;
-                lo->part[0].n_wg = first.wgs;
-                lo->part[1].n_slices = c.n;
-                lo->part[1].n_wg = c.wgs;
+                if (shared) put(&lo->part[0], first);
+                put(&lo->part[1], c);
             }
         }
     }
@@ -160,7 +185,7 @@ int prefix_layout(const ssv_prefix_params* p, PrefixLayout* lo) {
     own.rows = p->T * H_g;
     if (const int rc = plan_rows(&own, bf16, p->H_kv)) return rc;
     plan_slices(lo, p);
-    lo->n_slots = shared.n_slices + own.n_slices;
+    lo->n_slots = shared.slots + own.slots;
     lo->off_stats = 0;
     lo->off_acc = align_up((size_t)lo->n_slots * lo->rows_total * 8, 256);
     lo->total = align_up(lo->off_acc + (size_t)lo->n_slots * lo->rows_total * p->d_v * 4, 256);
@@ -202,7 +227,6 @@ int prefix_launch(const void* q, const void* kp, const void* vp, const void* k, 
     a.rows_total = lo.rows_total;
     a.div_TH = FastDiv::of(p->T * lo.H_g);
     a.div_Hg = FastDiv::of(lo.H_g);
-    a.div_Hkv = FastDiv::of(p->H_kv);
     for (int j = 0; j < 3; ++j) a.q_s[j] = lo.q_s[j];
     for (int own = 0; own < 2; ++own) {
         const PartPlan& pl = lo.part[own];
@@ -210,21 +234,23 @@ int prefix_launch(const void* q, const void* kp, const void* vp, const void* k, 
         pt.k = (const char*)(own ? k : kp);
         pt.v = (const char*)(own ? v : vp);
         pt.lens = own ? seq_lens : prefix_lens;
-        pt.per = pl.per; pt.rows = pl.rows; pt.n_rg = pl.n_rg;
+        pt.caches = pl.caches; pt.per = pl.per; pt.rows = pl.rows; pt.n_rg = pl.n_rg;
         pt.max_len = own ? p->max_seq_len : p->max_prefix_len;
-        pt.n_slices = pl.n_slices;
+        pt.units = pl.units; pt.slots = pl.slots; pt.min_tiles = pl.min_tiles;
+        pt.slot0 = own ? lo.part[0].slots : 0;
+        pt.by_length = pl.by_length;
+        pt.div_groups = FastDiv::of(p->H_kv * pl.n_rg);
         pt.div_rg = FastDiv::of(pl.n_rg);
-        pt.div_slices = FastDiv::of(pl.n_slices);
-        pt.slot0 = own ? lo.part[0].n_slices : 0;
-        pt.n_wg = pl.n_wg;
-        pt.n_pad = (int)align_up(pl.n_wg, 8);
+        pt.div_slices = FastDiv::of(pl.slots);
+        pt.n_wg = pl.units * p->H_kv * pl.n_rg;
+        pt.n_pad = (int)align_up(pt.n_wg, 8);
         for (int j = 0; j < 3; ++j) {
             pt.k_s[j] = (own ? p->k_stride : p->kp_stride)[j] * lo.es;
             pt.v_s[j] = (own ? p->v_stride : p->vp_stride)[j] * lo.es;
         }
     }
     // the prefix's rows are the own ones of one sequence or more: its path is the same or the next one up
-    const int own = lo.part[1].path, shared = lo.part[0].n_slices ? lo.part[0].path : own;
+    const int own = lo.part[1].path, shared = lo.part[0].units ? lo.part[0].path : own;
     constexpr int MANY = BF16 ? 0 : 2;
     const int rc = own == MANY      ? prefix_enqueue<BF16, DK, DV, MANY, MANY>(a, stream)
                    : shared == MANY ? prefix_enqueue<BF16, DK, DV, MANY, 1>(a, stream)
