@@ -203,6 +203,11 @@ def _ptr(t) -> Optional[int]:
     return t.data_ptr()
 
 
+def _ptrs(*tensors):
+    """_ptr of each.  One call for all arguments: acceptance and commit run in 2 to 4 us, and twelve calls take as long."""
+    return [t if t is None or t.__class__ is int else t.data_ptr() for t in tensors]
+
+
 def ssv_nsa_verify(q, k, v, k_cmp, v_cmp, gates, seq_lens, n_cmp, n_query, tree_parents, p: SsvNsaParams, out, sel_idx,
                    workspace, workspace_bytes: int, stream: int, kernel_ms=None, repeats: int = 1) -> None:
     """Enqueue one verification call on `stream` (a hipStream_t as an integer).
@@ -305,9 +310,8 @@ def ssv_prefix_workspace_bytes(p: SsvPrefixParams) -> int:
 def ssv_prefix_verify(q, k_prefix, v_prefix, k, v, prefix_lens, seq_lens, n_query, tree_parents, p: SsvPrefixParams, out,
                       workspace, workspace_bytes: int, stream: int) -> None:
     """Enqueue dense verification attention over shared prefixes and the sequences' own caches on `stream`."""
-    rc = load_library().ssv_prefix_verify(_ptr(q), _ptr(k_prefix), _ptr(v_prefix), _ptr(k), _ptr(v), _ptr(prefix_lens),
-                                          _ptr(seq_lens), _ptr(n_query), _ptr(tree_parents), ctypes.byref(p), _ptr(out),
-                                          _ptr(workspace), ctypes.c_size_t(int(workspace_bytes)), ctypes.c_void_p(int(stream)))
+    *inputs, to, space = _ptrs(q, k_prefix, v_prefix, k, v, prefix_lens, seq_lens, n_query, tree_parents, out, workspace)
+    rc = load_library().ssv_prefix_verify(*inputs, ctypes.byref(p), to, space, int(workspace_bytes), int(stream))
     if rc != SSV_OK:
         raise SsvError(rc, "ssv_prefix_verify")
 
@@ -325,9 +329,8 @@ def ssv_sample_workspace_bytes(p: SsvSampleParams) -> int:
 def ssv_sample(logits, temperature, top_k, top_p, min_p, u, n_query, p: SsvSampleParams, tokens, probs, workspace,
                workspace_bytes: int, stream: int) -> None:
     """Enqueue the sampling of one token per draft node from its logits and its given random number."""
-    rc = load_library().ssv_sample(_ptr(logits), _ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p), _ptr(u), _ptr(n_query),
-                                   ctypes.byref(p), _ptr(tokens), _ptr(probs), _ptr(workspace),
-                                   ctypes.c_size_t(int(workspace_bytes)), ctypes.c_void_p(int(stream)))
+    *inputs, to, to_probs, space = _ptrs(logits, temperature, top_k, top_p, min_p, u, n_query, tokens, probs, workspace)
+    rc = load_library().ssv_sample(*inputs, ctypes.byref(p), to, to_probs, space, int(workspace_bytes), int(stream))
     if rc != SSV_OK:
         raise SsvError(rc, "ssv_sample")
 
@@ -335,9 +338,8 @@ def ssv_sample(logits, temperature, top_k, top_p, min_p, u, n_query, p: SsvSampl
 def ssv_accept(draft_tokens, root_tokens, sampled, seq_lens, n_query, tree_parents, B: int, T: int, path, n_accepted, next_tokens,
                committed, stream: int) -> None:
     """Enqueue the walk through the drafts that the sampled tokens accept."""
-    rc = load_library().ssv_accept(_ptr(draft_tokens), _ptr(root_tokens), _ptr(sampled), _ptr(seq_lens), _ptr(n_query),
-                                   _ptr(tree_parents), int(B), int(T), _ptr(path), _ptr(n_accepted), _ptr(next_tokens),
-                                   _ptr(committed), ctypes.c_void_p(int(stream)))
+    inputs = _ptrs(draft_tokens, root_tokens, sampled, seq_lens, n_query, tree_parents)
+    rc = load_library().ssv_accept(*inputs, int(B), int(T), *_ptrs(path, n_accepted, next_tokens, committed), int(stream))
     if rc != SSV_OK:
         raise SsvError(rc, "ssv_accept")
 
@@ -351,7 +353,6 @@ def make_commit_params(*, layers=1, B, T, H_kv, d_k, d_v, dtype, kv_capacity, k_
 
 def ssv_commit(k, v, path, n_accepted, seq_lens, p: SsvCommitParams, stream: int) -> None:
     """Enqueue the move of the accepted draft rows of every layer to the front of the draft slots."""
-    rc = load_library().ssv_commit(_ptr(k), _ptr(v), _ptr(path), _ptr(n_accepted), _ptr(seq_lens), ctypes.byref(p),
-                                   ctypes.c_void_p(int(stream)))
+    rc = load_library().ssv_commit(*_ptrs(k, v, path, n_accepted, seq_lens), ctypes.byref(p), int(stream))
     if rc != SSV_OK:
         raise SsvError(rc, "ssv_commit")
