@@ -442,77 +442,35 @@ __global__ void __launch_bounds__(kSampleThreads) k_sample_pick(const SampleArgs
     const uint16_t* maxima = a.maxima + (int64_t)row * a.n_blocks * kSampleChunks;
     const int n_groups8 = a.n_blocks * (kSampleChunks / 8);
     const int n_it = (n_groups8 + kSampleThreads - 1) / kSampleThreads;
-    // body(iteration, first of this thread's eight chunks, their eight halves); chunks are in index order over (iteration, thread).  Four
-    // iterations' loads are in flight at a time.
+    // body(iteration, first of this thread's eight chunks, their eight halves); chunks are in index order over (iteration, thread).  The
+    // first HELD iterations' (vocabularies of up to 262144) are fetched once and stay in registers.
+    constexpr int HELD = 8;
+    auto fetch_max = [&](int it) { return *reinterpret_cast<const u32x4*>(maxima + 8 * min(it * kSampleThreads + tid, n_groups8 - 1)); };
+    u32x4 held[HELD];
+#pragma unroll
+    for (int k = 0; k < HELD; ++k) {
+        if (k >= n_it) break;             // (uniform)
+        held[k] = fetch_max(k);
+    }
     auto each_max = [&](auto&& body) {
-        for (int it0 = 0; it0 < n_it; it0 += 4) {
+        auto one = [&](int it, u32x4 x) {
+            const int g = it * kSampleThreads + tid;
+            body(it, 8 * g, g < n_groups8 ? x : u32x4{0, 0, 0, 0});
+        };
+#pragma unroll
+        for (int k = 0; k < HELD; ++k) {
+            if (k >= n_it) break;
+            one(k, held[k]);
+        }
+        for (int it0 = HELD; it0 < n_it; it0 += 4) {
             u32x4 x[4];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) x[k] = *reinterpret_cast<const u32x4*>(maxima + 8 * min((it0 + k) * kSampleThreads + tid, n_groups8 - 1));
+            for (int k = 0; k < 4; ++k) x[k] = fetch_max(it0 + k);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                if (it0 + k >= n_it) break;
-                const int g = (it0 + k) * kSampleThreads + tid;
-                body(it0 + k, 8 * g, g < n_groups8 ? x[k] : u32x4{0, 0, 0, 0});
-            }
+            for (int k = 0; k < 4; ++k)
+                if (it0 + k < n_it) one(it0 + k, x[k]);
         }
     };
-    uint32_t tau_m = 0;                      // min-p's threshold
-    if (rule.by_m) {
-        if (rule.min_p >= 1.f) {
-            tau_m = order_key(mx);
-        } else {
-            // the lowest key of weight min_p or more: within a few units of the key of M + t ln(min_p)
-            const uint32_t k0 = order_key((float)((double)mx + log((double)rule.min_p) * (double)rule.t));
-            const uint64_t reach = __builtin_amdgcn_ballot_w64(weight(key_value(k0 + (uint32_t)lane - 32u)) >= (double)rule.min_p);
-            tau_m = reach ? k0 + (uint32_t)__builtin_ctzll(reach) - 32u : order_key(mx);
-        }
-    }
-    const uint32_t lowest = order_key(-3.4028235e38f);      // (entries of -inf are never kept)
-    uint32_t lo = lowest;
-    if (rule.by_k) {
-        // the least of the maxima of as many groups of chunks, or of all chunks: as many logits are as large
-        uint32_t v[4] = {0, 0, 0, 0};
-        each_max([&](int, int, u32x4 x) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) v[j] = max(v[j], max(x[j] & 0xffffu, x[j] >> 16));
-        });
-        if (rule.top_k <= kSampleThreads) {      // (larger groups, and a higher bound)
-            v[0] = max(max(v[0], v[1]), max(v[2], v[3]));
-            v[1] = v[2] = v[3] = 0;
-        }
-        int count = 0, n_held;
-        uint32_t least = 0xffffu;
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-            if (v[j] >= lowest >> 16) {
-                ++count;
-                least = min(least, v[j]);
-            }
-        block_scan(count, s_int, tid, n_held);
-        if (n_held < rule.top_k) {
-            count = 0;
-            least = 0xffffu;
-            each_max([&](int, int, u32x4 x) {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const uint32_t half = j & 1 ? x[j >> 1] >> 16 : x[j >> 1] & 0xffffu;
-                    count += half >= lowest >> 16 ? 1 : 0;
-                    least = half >= lowest >> 16 ? min(least, half) : least;
-                }
-            });
-            block_scan(count, s_int, tid, n_held);
-        }
-        if (n_held >= rule.top_k) lo = (uint32_t)(0xffff - block_max((int)(0xffffu - least), s_int, tid)) << 16;
-    } else if (rule.by_p) {
-        // entries of weight below (1 - p) Z / V hold less than (1 - p) Z together
-        const double least = (1.0 - (double)rule.top_p) * (1.0 - 1e-9) * total / (double)a.V;
-        const uint32_t k = order_key(mx == INFINITY ? mx : (float)((double)mx + log(least) * (double)rule.t));
-        lo = max(lo, k > 2 ? k - 2 : 0);
-    }
-    if (rule.by_m && !rule.by_p) lo = max(lo, tau_m);
-    lo = max(lo, lowest);
-
     auto mass = [&](uint32_t k) { return (unsigned long long)(weight(key_value(k)) * a.mass_scale + 0.5); };
     auto clear_bins = [&] {
         if (tid < kSampleBins) {
@@ -560,6 +518,78 @@ __global__ void __launch_bounds__(kSampleThreads) k_sample_pick(const SampleArgs
         __syncthreads();
         return s_bin;
     };
+    uint32_t tau_m = 0;                      // min-p's threshold
+    if (rule.by_m) {
+        if (rule.min_p >= 1.f) {
+            tau_m = order_key(mx);
+        } else {
+            // the lowest key of weight min_p or more: within a few units of the key of M + t ln(min_p)
+            const uint32_t k0 = order_key((float)((double)mx + log((double)rule.min_p) * (double)rule.t));
+            const uint64_t reach = __builtin_amdgcn_ballot_w64(weight(key_value(k0 + (uint32_t)lane - 32u)) >= (double)rule.min_p);
+            tau_m = reach ? k0 + (uint32_t)__builtin_ctzll(reach) - 32u : order_key(mx);
+        }
+    }
+    const uint32_t lowest = order_key(-3.4028235e38f);      // (entries of -inf are never kept)
+    const uint32_t top_half = order_key(mx) >> 16;
+    // bins of equal width in halves, from the maximum's down over a range: 2^shift halves each; the lowest half of the bins up to f's
+    auto bin_shift = [](uint32_t range) { return range < (uint32_t)kSampleBins ? 0 : 32 - __builtin_clz(range) - __builtin_ctz(kSampleBins); };
+    auto bin_edge = [&](const BinFound& f, int shift) {
+        const uint32_t reach = (uint32_t)(f.bin + 1) << shift;
+        return f.reached && reach <= top_half ? top_half + 1 - reach : 0u;
+    };
+    uint32_t lo = lowest;
+    if (rule.by_k) {
+        // the k-th largest of the maxima of groups of chunks, four per thread (the lower edge of its bin): as many logits are as large.  With
+        // fewer groups the least of the maxima of all chunks, if there are k.
+        uint32_t v[4] = {0, 0, 0, 0};
+        each_max([&](int, int, u32x4 x) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] = max(v[j], max(x[j] & 0xffffu, x[j] >> 16));
+        });
+        int count = 0, n_held;
+        uint32_t least = 0xffffu;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (v[j] >= lowest >> 16) {
+                ++count;
+                least = min(least, v[j]);
+            }
+        block_scan(count, s_int, tid, n_held);
+        const bool by_groups = n_held >= rule.top_k;
+        if (!by_groups) {
+            count = 0;
+            least = 0xffffu;
+            each_max([&](int, int, u32x4 x) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const uint32_t half = j & 1 ? x[j >> 1] >> 16 : x[j >> 1] & 0xffffu;
+                    count += half >= lowest >> 16 ? 1 : 0;
+                    least = half >= lowest >> 16 ? min(least, half) : least;
+                }
+            });
+            block_scan(count, s_int, tid, n_held);
+        }
+        if (n_held >= rule.top_k) {
+            uint32_t edge = (uint32_t)(0xffff - block_max((int)(0xffffu - least), s_int, tid));
+            if (by_groups) {
+                const int shift = bin_shift(top_half - edge);
+                clear_bins();
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (v[j] >= edge) atomicAdd(&s_count[(top_half - v[j]) >> shift], 1u);
+                edge = max(edge, bin_edge(find_bin(false, (uint32_t)rule.top_k, 0.0), shift));
+            }
+            lo = edge << 16;
+        }
+    } else if (rule.by_p) {
+        // entries of weight below (1 - p) Z / V hold less than (1 - p) Z together
+        const double least = (1.0 - (double)rule.top_p) * (1.0 - 1e-9) * total / (double)a.V;
+        const uint32_t k = order_key(mx == INFINITY ? mx : (float)((double)mx + log(least) * (double)rule.t));
+        lo = max(lo, k > 2 ? k - 2 : 0);
+    }
+    if (rule.by_m && !rule.by_p) lo = max(lo, tau_m);
+    lo = max(lo, lowest);
+
     // ---- the candidates, in index order.  First chunks whose maximum (its upper half's upper end) reaches a bound, then their logits.
     uint64_t* s_list = reinterpret_cast<uint64_t*>(s_mem);
     uint32_t* s_chunk = reinterpret_cast<uint32_t*>(s_sorted);
@@ -613,14 +643,12 @@ __global__ void __launch_bounds__(kSampleThreads) k_sample_pick(const SampleArgs
         __syncthreads();
         return n_hit;
     };
-    // Of these, by bins of equal width in halves from the maximum's down: where the chunks' maxima alone (their lower ends) suffice,
-    // nothing beyond that bin is kept.
-    const uint32_t top_half = order_key(mx) >> 16;
+    // Of these, by bins of equal width in halves: where the chunks' maxima alone (their lower ends) suffice, nothing beyond that bin is
+    // kept.  (By count the bound is as good already, unless the list is too long.)
     uint32_t half = lo >> 16;
     int n_hit = list_chunks(half);
-    if (rule.by_k || rule.by_p) {
-        int shift = 0;
-        while ((top_half - half) >> shift >= kSampleBins) ++shift;
+    if (n_hit > kSampleList ? rule.by_k || rule.by_p : rule.by_p && !rule.by_k) {
+        const int shift = bin_shift(top_half - half);
         clear_bins();
         auto count = [&](uint32_t h) {
             if (h << 16 < lo) return;
@@ -639,12 +667,8 @@ __global__ void __launch_bounds__(kSampleThreads) k_sample_pick(const SampleArgs
                 }
             });
         }
-        const BinFound f = find_bin(!rule.by_k, (uint32_t)rule.top_k, (double)rule.top_p * (1.0 + 1e-9) * total * a.mass_scale);
-        if (f.reached) {
-            const uint32_t edge = top_half + 1 - ((uint32_t)(f.bin + 1) << shift);      // (bins up to it hold the halves from here on)
-            if ((uint32_t)(f.bin + 1) << shift <= top_half) half = max(half, edge);
-            lo = max(lo, half << 16);
-        }
+        half = max(half, bin_edge(find_bin(!rule.by_k, (uint32_t)rule.top_k, (double)rule.top_p * (1.0 + 1e-9) * total * a.mass_scale), shift));
+        lo = max(lo, half << 16);
     }
     if (n_hit > kSampleList) n_hit = list_chunks(half);
     bool listed = n_hit <= kSampleList;
