@@ -315,6 +315,19 @@ __device__ __forceinline__ V block_max(V x, V* s_part, int tid) {
     return x;
 }
 
+// Descending over the lanes: a bitonic sort through lane exchanges.
+__device__ __forceinline__ uint64_t wave_sort(uint64_t x, int lane) {
+#pragma unroll
+    for (int run = 2; run <= 64; run *= 2)
+#pragma unroll
+        for (int gap = run / 2; gap; gap /= 2) {
+            const uint64_t y = __shfl_xor(x, gap);
+            const bool larger = ((lane & gap) == 0) == ((lane & run) == 0);      // this lane keeps the larger one
+            x = (x > y) == larger ? x : y;
+        }
+    return x;
+}
+
 // A list entry: larger is earlier in the order (logit descending, index ascending).
 __device__ __forceinline__ uint64_t list_entry(uint32_t key, int e) { return (uint64_t)key << 32 | (0xffffffffu - (uint32_t)e); }
 __device__ __forceinline__ float entry_value(uint64_t x) { return key_value((uint32_t)(x >> 32)); }
@@ -329,7 +342,6 @@ __global__ void __launch_bounds__(kSampleThreads) k_sample_pick(const SampleArgs
     __shared__ unsigned long long s_mass[kSampleBins], s_above, s_part64[kSampleWaves];
     __shared__ uint32_t s_count[kSampleBins], s_digit;
     __shared__ double s_part[kSampleWaves];
-    __shared__ float s_float[kSampleWaves];
     __shared__ int s_int[kSampleWaves];
     __shared__ BinFound s_bin;
     static_assert(kSampleMaxIters * kSampleWaves * 12 + 256 * 8 <= sizeof(s_mem) && kSampleMaxBlocks * 8 <= sizeof(s_mem), "one array for every way");
@@ -353,9 +365,10 @@ __global__ void __launch_bounds__(kSampleThreads) k_sample_pick(const SampleArgs
     float u = a.u[row];
     u = u >= 0.f ? fminf(u, 1.f) : 0.f;
 
+    // (every wavefront for itself: a barrier takes longer than the blocks of a row)
     float mx = -INFINITY;
-    for (int k = tid; k < a.n_blocks; k += kSampleThreads) mx = fmaxf(mx, (float)blocks[k].max);
-    mx = block_max(mx, s_float, tid);
+    for (int k = lane; k < a.n_blocks; k += 64) mx = fmaxf(mx, (float)blocks[k].max);
+    mx = wave_max(mx);
     if (mx == -INFINITY) {
         if (tid == 0) {
             *token = -1;
@@ -364,20 +377,19 @@ __global__ void __launch_bounds__(kSampleThreads) k_sample_pick(const SampleArgs
         return;
     }
     if (rule.first) {
+        if (wave) return;
         int at = -0x7fffffff;      // minus the first block that holds the maximum
-        for (int k = tid; k < a.n_blocks; k += kSampleThreads)
+        for (int k = lane; k < a.n_blocks; k += 64)
             if ((float)blocks[k].max == mx) at = max(at, -k);
-        at = -block_max(at, s_int, tid);
+        const int c = -wave_max(at) * kSampleChunks + lane * (kSampleChunks / 64);
+        float x[kSampleChunks / 64][8];
+        logits.load_each(c, 1, x);
         int e = -0x7fffffff;
-        if (tid < kSampleChunks) {
-            float x[8];
-            logits.load(at * kSampleChunks + tid, x);
 #pragma unroll
-            for (int j = 7; j >= 0; --j)
-                if (x[j] == mx) e = -(logits.first(at * kSampleChunks + tid) + j);
-        }
-        e = -block_max(e, s_int, tid);
-        if (tid == 0) {
+        for (int k = 8 * (kSampleChunks / 64) - 1; k >= 0; --k)
+            if (x[k >> 3][k & 7] == mx) e = -(logits.first(c) + k);
+        e = -wave_max(e);
+        if (lane == 0) {
             *token = e;
             if (prob) *prob = 1.f;
         }
@@ -389,17 +401,17 @@ __global__ void __launch_bounds__(kSampleThreads) k_sample_pick(const SampleArgs
     double* s_sum = reinterpret_cast<double*>(s_mem);
     double total = 0.0;
     if (rule.sums()) {
-        double sum = 0.0;
-        for (int k = tid; k < a.n_blocks; k += kSampleThreads) {
+        for (int k = lane; k < a.n_blocks; k += 64) {
             const SampleBlock x = blocks[k];
             const double v = x.sum == 0.0 ? 0.0 : x.sum * weight.of_block(x.max);
-            s_sum[k] = v;
-            sum += v;
+            if (wave == 0) s_sum[k] = v;
+            total += v;
         }
-        block_scan(sum, s_part, tid, total);
+        total = wave_sum(total);
     }
     if (!rule.filters()) {
         if (wave) return;
+        __builtin_amdgcn_wave_barrier();
         const Found<double> f = find_prefix(s_sum, a.n_blocks, lane, [&](double all) { return (double)u * all; });
         const double target = (double)u * f.total;
         const bool past = u >= 1.f || f.before >= f.total;      // nothing exceeds the target: the last positive weight
@@ -728,46 +740,56 @@ __global__ void __launch_bounds__(kSampleThreads) k_sample_pick(const SampleArgs
     const float width = mx - key_value(lo);
     const float inv = width > 0.f && width < INFINITY ? (float)kSampleBins / width : 0.f;
     auto bin_of = [&](float x) { return x == mx ? 0 : min(kSampleBins - 1, (int)((mx - x) * inv)); };
+    if (listed && n <= 64) {
+        // ---- one wavefront, an entry per lane, no barriers
+        if (wave) return;
+        const uint64_t entry = lane < n ? s_list[lane] : 0ull;
+        uint64_t last_kept = 0;
+        if (rule.by_k || rule.by_p) {
+            const uint64_t x = wave_sort(entry, lane);
+            int kept = rule.by_k ? min(rule.top_k, n) : n;
+            if (rule.by_p) {
+                const double cum = wave_incl_scan(lane < n ? weight(entry_value(x)) : 0.0);
+                const double target = (double)rule.top_p * (rule.by_k ? __shfl(cum, kept - 1) : total);
+                kept = min(kept, 1 + __builtin_popcountll(__builtin_amdgcn_ballot_w64(lane < kept && cum < target)));
+            }
+            last_kept = __shfl(x, kept - 1);
+        }
+        const double w = lane < n && entry >= last_kept && (uint32_t)(entry >> 32) >= tau_m ? weight(entry_value(entry)) : 0.0;
+        const double cum = wave_incl_scan(w), all = last_lane(cum);
+        const uint64_t over = u < 1.f ? __builtin_amdgcn_ballot_w64(w > 0.0 && cum > (double)u * all) : 0ull;
+        const uint64_t some = __builtin_amdgcn_ballot_w64(w > 0.0);
+        if (lane == (over ? __builtin_ctzll(over) : 63 - __builtin_clzll(some | 1ull))) {
+            *token = entry_index(entry);
+            if (prob) *prob = (float)(w / all);
+        }
+        return;
+    }
     const int q = (n + kSampleThreads - 1) / kSampleThreads, l0 = min(n, tid * q), l1 = min(n, l0 + q);     // this thread's entries
     uint64_t last_kept = 0;             // the last entry that is kept
     if (listed && (rule.by_k || rule.by_p)) {
         // ---- the exact threshold: a histogram of the list, and the entries of the bin in which it falls in order
-        const bool whole = n <= 64;          // one wavefront's sort takes the whole list
-        if (!whole) {
-            clear_bins();
-            for (int l = l0; l < l1; ++l) {
-                const uint32_t key = (uint32_t)(s_list[l] >> 32);
-                const int at = bin_of(key_value(key));
-                atomicAdd(&s_count[at], 1u);
-                if (rule.by_p) atomicAdd(&s_mass[at], mass(key));
-            }
+        clear_bins();
+        for (int l = l0; l < l1; ++l) {
+            const uint32_t key = (uint32_t)(s_list[l] >> 32);
+            const int at = bin_of(key_value(key));
+            atomicAdd(&s_count[at], 1u);
+            if (rule.by_p) atomicAdd(&s_mass[at], mass(key));
         }
-        const BinFound all_of_it{0, 1, 0u, 0ull};
         // the entries of a bin into s_sorted, descending; how many
         auto sort_bin = [&](int bin) {
             int mine = 0, m;
-            for (int l = l0; l < l1; ++l) mine += whole || bin_of(entry_value(s_list[l])) == bin ? 1 : 0;
+            for (int l = l0; l < l1; ++l) mine += bin_of(entry_value(s_list[l])) == bin ? 1 : 0;
             int at = block_scan(mine, s_int, tid, m);
             if (m > kSampleSort) return m;
             for (int l = l0; l < l1; ++l)
-                if (whole || bin_of(entry_value(s_list[l])) == bin) s_sorted[at++] = s_list[l];
+                if (bin_of(entry_value(s_list[l])) == bin) s_sorted[at++] = s_list[l];
             int size = 64;
             while (size < m) size *= 2;
             for (int k = m + tid; k < size; k += kSampleThreads) s_sorted[k] = 0ull;
             __syncthreads();
             if (size == 64) {              // one wavefront, by lane exchanges
-                if (wave == 0) {
-                    uint64_t x = s_sorted[lane];
-#pragma unroll
-                    for (int run = 2; run <= 64; run *= 2)
-#pragma unroll
-                        for (int gap = run / 2; gap; gap /= 2) {
-                            const uint64_t y = __shfl_xor(x, gap);
-                            const bool larger = ((lane & gap) == 0) == ((lane & run) == 0);      // this lane keeps the larger one
-                            x = (x > y) == larger ? x : y;
-                        }
-                    s_sorted[lane] = x;
-                }
+                if (wave == 0) s_sorted[lane] = wave_sort(s_sorted[lane], lane);
                 __syncthreads();
                 return m;
             }
@@ -802,7 +824,7 @@ __global__ void __launch_bounds__(kSampleThreads) k_sample_pick(const SampleArgs
         double target = (double)rule.top_p * total * a.mass_scale;
         bool done = false;
         if (rule.by_k) {
-            const BinFound f = whole ? all_of_it : find_bin(false, (uint32_t)rule.top_k, 0.0);
+            const BinFound f = find_bin(false, (uint32_t)rule.top_k, 0.0);
             const int m = sort_bin(f.bin);
             listed = m <= kSampleSort;
             if (listed) {
@@ -820,7 +842,7 @@ __global__ void __launch_bounds__(kSampleThreads) k_sample_pick(const SampleArgs
             }
         }
         if (rule.by_p && listed && !done) {
-            const BinFound f = whole ? all_of_it : find_bin(true, 0u, target);
+            const BinFound f = find_bin(true, 0u, target);
             const int m = sort_bin(f.bin);
             listed = m <= kSampleSort;
             if (listed) {
