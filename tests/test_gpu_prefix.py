@@ -209,3 +209,70 @@ def test_offsets_beyond_32_bits():
     f = lambda x: x.double().numpy()
     check(args, dict(q=f(q), kp=f(hk)[None, None], vp=f(hv)[None, None], k=f(k), v=f(v), plens=[rows], lens=[0, 0], nq=[1, 1], parents=None,
                      scale=dk ** -0.5, dk=dk, dt="bf16"))
+
+
+@pytest.mark.parametrize("shape", ["bf16_192", "f32_64"])
+@pytest.mark.parametrize("lens", [[1500, 0, 0, 1, 3, 700, 2], [0] * 7, [64, 128, 192, 65, 127, 1, 0], [5, 5, 5, 5, 5, 5, 1023]], ids=str)
+def test_slices_dealt_out_by_length(shape, lens):
+    """One sequence or prefix much longer than the others, none, and lengths on the tile borders; sequences without nodes."""
+    nq = [2, 0, 1, 2, 2, 2, 0]
+    args, h = setup(18, shape, B=7, T=2, H=4, Hk=2, G=7, plens=[lens[-1 - i] for i in range(7)], lens=lens, nq=nq, P=1500, S=1500)
+    call(args)
+    check(args, h)
+    args, h = setup(19, shape, B=7, T=2, H=4, Hk=2, G=1, plens=[333], lens=lens, nq=nq, S=1500)
+    call(args)
+    check(args, h)
+
+
+@pytest.mark.parametrize("B", [63, 64, 65, 130])
+def test_batches_around_one_cache_per_lane(B):
+    rng = np.random.default_rng(B)
+    args, h = setup(20, "bf16_64", B=B, T=1, H=2, Hk=1, G=1, plens=[77], lens=[int(x) for x in rng.integers(0, 200, B)])
+    call(args)
+    check(args, h)
+    args, h = setup(21, "bf16_64", B=B, T=1, H=2, Hk=2, G=B, plens=[int(x) for x in rng.integers(0, 150, B)], lens=[int(x) for x in rng.integers(0, 20, B)])
+    call(args)
+    check(args, h)
+
+
+def test_long_prefix_of_few_rows_and_many_slices():
+    """One row against many keys (as many slices as there are slots) and a window of nothing but the node itself."""
+    args, h = setup(22, "bf16_192", B=1, T=1, H=1, Hk=1, G=1, plens=[9000], lens=[0])
+    call(args)
+    check(args, h)
+    args, h = setup(23, "bf16_128", B=1, T=2, H=16, Hk=1, G=1, plens=[9000], lens=[5000])
+    call(args)
+    check(args, h)
+
+
+def test_two_calls_on_two_streams():
+    """Calls with workspaces of their own may overlap."""
+    import torch
+    sets = [setup(30 + k, "bf16_128", B=3, T=4, H=8, Hk=2, G=1, plens=[700 + k], lens=[40, 0, 9]) for k in range(2)]
+    streams = [torch.cuda.Stream() for _ in sets]
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for (args, _), s in zip(sets, streams):
+            with torch.cuda.stream(s):
+                call(args)
+    torch.cuda.synchronize()
+    for args, h in sets:
+        check(args, h)
+
+
+def test_fuzz_of_small_problems():
+    """Drawn shapes, lengths, trees and counts."""
+    rng = np.random.default_rng(99)
+    for case in range(40):
+        shape = str(rng.choice(sorted(SHAPES)))
+        G = int(rng.choice([1, 1, 2, 3]))
+        B, T = G * int(rng.integers(1, 6)), int(rng.choice([1, 1, 2, 5, 17, 33]))
+        Hk, Hg = int(rng.choice([1, 2, 3])), int(rng.choice([1, 2, 4, 8, 16]))
+        par = None if rng.random() < 0.5 else [int(rng.integers(max(-1, i - 3), i)) for i in range(T)]
+        top = int(rng.choice([3, 70, 300]))
+        print("case", case, shape, B, T, Hk, Hg, G, top, flush=True)
+        args, h = setup(1000 + case, shape, B=B, T=T, H=Hk * Hg, Hk=Hk, G=G, plens=[int(x) for x in rng.integers(0, top + 1, G)],
+                        lens=[int(x) for x in rng.integers(0, top + 1, B)], nq=[int(x) for x in rng.integers(0, T + 1, B)], parents=par,
+                        P=top, S=top, strided=bool(rng.random() < 0.3))
+        call(args)
+        check(args, h)

@@ -186,3 +186,43 @@ def test_frequencies_follow_the_probabilities():
     share = np.zeros(50)
     share[order[keep]] = w[order[keep]] / w[order[keep]].sum()
     assert (np.abs(np.bincount(tok[0], minlength=50) - n * share) <= 1.0 + 1e-6).all()
+
+
+def test_lists_of_every_length():
+    """Kept entries around what one wavefront solves, what is sorted and what is listed, and the general way beyond: flat rows, where
+    the thresholds fall among thousands of candidates, by count, by mass and by both."""
+    rng = np.random.default_rng(51)
+    V = 50021
+    for dt in ("f32", "bf16"):
+        x = 0.3 * logits(51, (10, 2, V), dt, tail=0.0)
+        k = [60, 64, 65, 500, 1100, 2047, 2600, 4000, 9000, 30000]
+        check(x, [1.0] * 10, k, [1.0] * 10, [0.0] * 10, rng.random((10, 2)))
+        check(x, [1.0] * 10, k, [0.8, 0.99, 0.5, 0.9, 0.7, 0.97, 0.3, 0.9, 0.6, 0.999], [0.0] * 5 + [0.2] * 5, rng.random((10, 2)))
+        check(x, [1.0] * 10, [0] * 10, [0.0005, 0.002, 0.01, 0.04, 0.1, 0.3, 0.5, 0.8, 0.95, 0.9999], [0.0] * 10, rng.random((10, 2)))
+        check(x, [1.0] * 10, [0] * 10, [1.0] * 10, [0.9, 0.8, 0.7, 0.6, 0.5, 0.4, 0.3, 0.2, 0.1, 0.01], rng.random((10, 2)))
+
+
+def test_masked_vocabularies():
+    """Most of the vocabulary at -inf: fewer entries than top-k, whole blocks without one."""
+    import torch
+    x = logits(52, (6, 1, 40000), "bf16")
+    x[:, :, 100:39990] = float("-inf")
+    x[3, :, 5:] = float("-inf")
+    x[4, :, :39999] = float("-inf")
+    x[5] = torch.where(torch.rand((1, 40000), device="cuda") < 0.9, float("-inf"), x[5])
+    for s in SETTINGS:
+        check(x, [s[0]] * 6, [s[1]] * 6, [s[2]] * 6, [s[3]] * 6, np.random.default_rng(52).random((6, 1)))
+
+
+def test_largest_vocabulary_and_many_rows():
+    import torch
+    from paper_2605_19893_amd import binding as Bd
+    V = Bd.SSV_SAMPLE_MAX_V
+    x = logits(53, (4, 1, V), "f32")
+    rng = np.random.default_rng(53)
+    check(x, [1.0, 0.7, 0.9, 3.0], [0, 50, 0, 3000], [1.0, 0.9, 0.95, 0.9], [0.0, 0.0, 0.0, 0.0], rng.random((4, 1)))
+    y = torch.zeros(V + 5, dtype=torch.bfloat16, device="cuda")[5:].reshape(1, 1, V)       # an unaligned row of equal logits
+    check(y, [1.0], [0], [0.5], [0.0], [[0.7]])
+    x = logits(54, (700, 3, 257), "bf16")
+    n = 700
+    check(x, [0.9] * n, [0 if i % 3 else 7 for i in range(n)], [0.9 if i % 2 else 1.0 for i in range(n)], [0.0] * n, rng.random((n, 3)))
