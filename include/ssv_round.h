@@ -33,7 +33,7 @@ typedef struct ssv_prefix_params {
     int32_t max_seq_len;      /* host-side bound on seq_lens[b]; k and v hold at least max_seq_len + T rows per (sequence, KV head) */
     int64_t kp_stride[3], vp_stride[3];   /* elements: prefix, KV head, row */
     int64_t k_stride[3], v_stride[3];     /* elements: sequence, KV head, row */
-    int64_t q_stride[3], out_stride[3];   /* elements: sequence, node, head; all zero = contiguous [B,T,H,d] */
+    int64_t q_stride[3], out_stride[3];   /* elements: sequence, node, head; all zero = contiguous [B,T,H,d]; rows of out do not overlap */
 } ssv_prefix_params;
 
 /*
@@ -114,7 +114,7 @@ typedef struct ssv_commit_params {
     int32_t d_k, d_v;         /* row lengths; times the element size multiples of 16 bytes */
     int32_t dtype;            /* SSV_F32 or SSV_BF16 */
     int32_t kv_capacity;      /* rows of k / v per (layer, sequence, KV head) */
-    int64_t k_stride[4], v_stride[4];   /* elements: layer, sequence, KV head, row; multiples of 16 bytes */
+    int64_t k_stride[4], v_stride[4];   /* elements: layer, sequence, KV head, row; multiples of 16 bytes; caches do not overlap */
 } ssv_commit_params;
 
 /*

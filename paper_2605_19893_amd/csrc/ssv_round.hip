@@ -21,6 +21,9 @@ constexpr int kMaxDevices = 64;   // per-device one-time set-up flags
 int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 bool misaligned(const void* p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to != 0; }
+bool launchable(int64_t workgroups, int threads) { return workgroups * threads < (1ll << 32); }      // threads of a launch are counted in 32 bits
+// Strides of something written in place: distinct indices are distinct places.
+bool repeats(int64_t extent, int64_t stride) { return extent > 1 && stride == 0; }
 
 // ---- shared-prefix attention
 constexpr int kPrefixMaxSlices = kPrefixMaxSlots / 2;      // per part (prefix, own rows)
@@ -46,7 +49,7 @@ int plan_rows(PartPlan* pt, bool bf16, int H_kv) {
     pt->by_length = pt->caches > 1 && pt->caches <= kPrefixMaxDealt;
     pt->path = pt->rows <= 16 ? 1 : (bf16 ? 0 : 2);
     pt->n_rg = ceil_div(pt->rows, pt->path ? 16 * pt->path : 256);
-    return (int64_t)pt->caches * H_kv * pt->n_rg * kPrefixMaxSlices > (1 << 24) ? SSV_EUNSUPPORTED : SSV_OK;
+    return launchable(2 * ((int64_t)pt->caches * H_kv * pt->n_rg * kPrefixMaxSlices + 8), kPrefixThreads) ? SSV_OK : SSV_EUNSUPPORTED;
 }
 
 // What a part would cost in a number of slices: workgroups, and microseconds of the longest and of an average one.  A rough model
@@ -167,10 +170,11 @@ int prefix_layout(const ssv_prefix_params* p, PrefixLayout* lo) {
         }
         if (!dense && st[2] < dd[s] && p->H > 1) return SSV_EINVAL;
     }
+    if (repeats(p->B, lo->out_s[0]) || repeats(p->T, lo->out_s[1])) return SSV_EINVAL;
     lo->H_g = H_g;
     lo->es = es;
     lo->rows_total = (int64_t)p->B * p->T * p->H;
-    if (lo->rows_total >= (1ll << 31)) return SSV_EUNSUPPORTED;
+    if (!launchable(lo->rows_total + kThreads, p->d_v / 4)) return SSV_EUNSUPPORTED;      // (k_prefix_combine; sizes fit 31 bits)
     const bool bf16 = p->dtype == SSV_BF16;
     PartPlan& shared = lo->part[0];
     if (p->max_prefix_len) {
@@ -275,7 +279,9 @@ int sample_check(const ssv_sample_params* p, int64_t s[2]) {
     if (!p || p->B < 1 || p->T < 1 || p->V < 1) return SSV_EINVAL;
     if (p->dtype != SSV_F32 && p->dtype != SSV_BF16) return SSV_EINVAL;
     if (p->logits_stride[0] < 0 || p->logits_stride[1] < 0) return SSV_EINVAL;
-    if (p->V > SSV_SAMPLE_MAX_V || (int64_t)p->B * p->T * sample_blocks(p->V) >= (1ll << 28)) return SSV_EUNSUPPORTED;
+    const int64_t rows = (int64_t)p->B * p->T;
+    if (p->V > SSV_SAMPLE_MAX_V || !launchable(rows, kSampleThreads) ||
+        !launchable(rows * ceil_div(sample_blocks(p->V), kThreads / 64), kThreads)) return SSV_EUNSUPPORTED;
     const int es = p->dtype == SSV_BF16 ? 2 : 4;
     const bool dense = !p->logits_stride[0] && !p->logits_stride[1];
     s[0] = (dense ? (int64_t)p->T * p->V : p->logits_stride[0]) * es;
@@ -371,7 +377,7 @@ int ssv_accept(const int32_t* draft_tokens, const int32_t* root_tokens, const in
                const int32_t* n_query, const int32_t* tree_parents, int32_t B, int32_t T, int32_t* path, int32_t* n_accepted,
                int32_t* next_tokens, int32_t* committed, void* stream) {
     if (B < 1 || T < 1) return SSV_EINVAL;
-    if (T > SSV_MAX_T) return SSV_EUNSUPPORTED;
+    if (T > SSV_MAX_T || !launchable(ceil_div(B, kThreads / 64), kThreads)) return SSV_EUNSUPPORTED;
     if (!draft_tokens || !root_tokens || !sampled || !seq_lens || !path || !n_accepted || !next_tokens || !committed) return SSV_EINVAL;
     const void* words[] = {draft_tokens, root_tokens, sampled, seq_lens, n_query, tree_parents, path, n_accepted, next_tokens, committed};
     for (const void* w : words)
@@ -393,6 +399,8 @@ int ssv_commit(void* k, void* v, const int32_t* path, const int32_t* n_accepted,
         for (int j = 0; j < 4; ++j) {
             if (strides[s][j] < 0 || strides[s][j] * es % 16) return SSV_EINVAL;
             if (j == 3 && strides[s][j] < (s ? p->d_v : p->d_k)) return SSV_EINVAL;
+            const int extents[4] = {p->layers, p->B, p->H_kv, 1};
+            if (repeats(extents[j], strides[s][j])) return SSV_EINVAL;
         }
     if (!k || !v || !path || !n_accepted || !seq_lens || misaligned(k, 16) || misaligned(v, 16)) return SSV_EINVAL;
     if (misaligned(path, 4) || misaligned(n_accepted, 4) || misaligned(seq_lens, 4)) return SSV_EINVAL;
@@ -403,7 +411,7 @@ int ssv_commit(void* k, void* v, const int32_t* path, const int32_t* n_accepted,
     a.k_chunks = p->d_k * es / 16;
     a.chunks = a.k_chunks + p->d_v * es / 16;
     const int64_t pairs = (int64_t)p->layers * p->B * p->H_kv;
-    if (pairs >= (1ll << 31) || pairs * a.chunks >= (1ll << 38)) return SSV_EUNSUPPORTED;
+    if (pairs >= (1ll << 31) || !launchable(pairs, a.chunks) || !launchable(ceil_div(pairs * a.chunks, kThreads), kThreads)) return SSV_EUNSUPPORTED;
     a.total = pairs * a.chunks;
     for (int j = 0; j < 4; ++j) {
         a.k_s[j] = p->k_stride[j] * es;

@@ -196,3 +196,34 @@ def test_definition_of_attention_equals_one_softmax_over_all_rows():
     p = np.exp(0.5 * q[0, 1, 1] @ keys.T)
     assert np.allclose(out[0, 1, 1], p @ vals / p.sum())
     assert (out[1, 1] == 0).all() and (mass >= np.abs(out) - 1e-12).all()
+
+
+@pytest.mark.parametrize("over, code", [
+    (dict(out_stride=(0, 64 * 128, 128)), B.SSV_EINVAL), (dict(out_stride=(8 * 64 * 128, 0, 128)), B.SSV_EINVAL),
+    (dict(B=1 << 14, T=128, n_prefix=1), B.SSV_EUNSUPPORTED), (dict(B=1 << 18, T=1, n_prefix=1 << 18), B.SSV_EUNSUPPORTED)])
+def test_prefix_refuses_repeated_rows_and_launches_beyond_32_bits(over, code):
+    test_prefix_refusals(over, code)
+
+
+def test_prefix_accepts_broadcast_inputs():
+    for over in (dict(k_stride=(0, 0, 192), v_stride=(0, 0, 128)), dict(kp_stride=(0, 0, 192), vp_stride=(0, 0, 128)), dict(q_stride=(0, 0, 192)),
+                 dict(B=1, n_prefix=1, T=1, out_stride=(0, 0, 128))):
+        assert B.ssv_prefix_workspace_bytes(prefix_params(**over)) > 0
+
+
+def test_launches_beyond_32_bits_are_refused():
+    """The threads of a launch are counted in 32 bits."""
+    assert B.ssv_sample_workspace_bytes(B.make_sample_params(B=(1 << 23) - 1, T=1, V=1, dtype=B.SSV_F32)) > 0
+    test_sample_refusals(dict(B=1 << 23, T=1, V=1), B.SSV_EUNSUPPORTED)
+    test_sample_refusals(dict(B=1 << 21, T=1, V=60000), B.SSV_EUNSUPPORTED)
+    with pytest.raises(B.SsvError) as e:
+        B.ssv_accept(*[P16] * 6, 1 << 26, 3, *[P16] * 4, 0)
+    assert e.value.code == B.SSV_EUNSUPPORTED
+    test_commit_refusals(dict(layers=1 << 12, B=1 << 10, H_kv=1 << 6), B.SSV_EUNSUPPORTED)
+
+
+@pytest.mark.parametrize("at", [0, 1, 2])
+def test_commit_refuses_caches_at_one_place(at):
+    good = (25600, 12800, 6400, 64)
+    test_commit_refusals(dict(k_stride=good[:at] + (0,) + good[at + 1:]), B.SSV_EINVAL)
+    test_commit_refusals(dict(v_stride=good[:at] + (0,) + good[at + 1:]), B.SSV_EINVAL)
