@@ -98,12 +98,12 @@ __device__ __forceinline__ bool whole_exponents(double M, double c) { return M -
 struct SampleWeight {
     double M, c;       // c = log2(e) / temperature
     float Mf;
-    __device__ __forceinline__ double operator()(float x) const { return x == Mf ? 1.0 : exp2_64(((double)x - M) * c); }
+    __device__ __forceinline__ double operator()(float x) const { return exp2_64(x == Mf ? 0.0 : ((double)x - M) * c); }
     // of a block of sum 1
     __device__ __forceinline__ double of_block(double max) const {
         if (!whole_exponents(max, c)) return (*this)((float)max);
         const double e = __builtin_rint(max * c);
-        return whole_exponents(M, c) ? exp2_64((e - M * c)) : exp2_64((max - M) * c + (e - max * c));
+        return exp2_64(whole_exponents(M, c) ? e - M * c : (max - M) * c + (e - max * c));
     }
 };
 
@@ -159,35 +159,51 @@ struct SampleRow {
         }
         return r;
     }
+    // The chunks at the ends of the row and beyond, by elements (in a loop of its own: the code is fetched more often than it runs).
+    __device__ __forceinline__ void ends(int c, Raw& r) const {
+        if (c >= lo && c < hi) return;
+        uint32_t w[8 * ES / 4];
+#pragma unroll
+        for (int k = 0; k < 8 * ES / 4; ++k) w[k] = 0;
+#pragma unroll 1
+        for (int j = 0; j < 8; ++j) {
+            const int e = first(c) + j;
+            const bool in = e >= 0 && e < V;
+#pragma unroll
+            for (int k = 0; k + 1 < 8 * ES / 4; ++k) w[k] = BF16 ? __builtin_amdgcn_alignbit(w[k + 1], w[k], 16) : w[k + 1];
+            uint32_t& last = w[8 * ES / 4 - 1];
+            if constexpr (BF16) last = last >> 16 | (uint32_t)(in ? reinterpret_cast<const uint16_t*>(base)[e] : 0xff80u) << 16;
+            else last = in ? reinterpret_cast<const uint32_t*>(base)[e] : 0xff800000u;
+        }
+#pragma unroll
+        for (int k = 0; k < 8 * ES / 4; ++k) r.v[k >> 2][k & 3] = w[k];
+    }
     template <bool CLEAN = true>
-    __device__ __forceinline__ void unpack(int c, const Raw& r, float (&x)[8]) const {
+    __device__ __forceinline__ void unpack(const Raw& r, float (&x)[8]) const {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             if constexpr (BF16) x[j] = __uint_as_float(j & 1 ? r.v[0][j >> 1] & 0xffff0000u : r.v[0][j >> 1] << 16);
             else x[j] = __uint_as_float(r.v[j >> 2][j & 3]);
         }
-        if (c < lo || c >= hi) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const int e = first(c) + j;
-                x[j] = -INFINITY;
-                if (e >= 0 && e < V) {
-                    if constexpr (BF16) x[j] = __uint_as_float((uint32_t)reinterpret_cast<const uint16_t*>(base)[e] << 16);
-                    else x[j] = reinterpret_cast<const float*>(base)[e];
-                }
-            }
-        }
 #pragma unroll
         for (int j = 0; j < 8; ++j) x[j] = CLEAN ? clean(x[j]) : x[j] + 0.f;      // (either way no signalling NaN)
     }
-    __device__ __forceinline__ void load(int c, float (&x)[8]) const { unpack(c, fetch(c), x); }
+    __device__ __forceinline__ void load(int c, float (&x)[8]) const {
+        Raw r = fetch(c);
+        ends(c, r);
+        unpack(r, x);
+    }
     template <bool CLEAN = true, int N>
     __device__ __forceinline__ void load_each(int c, int step, float (&x)[N][8]) const {      // chunks c, c + step, ...
         Raw r[N];
 #pragma unroll
         for (int k = 0; k < N; ++k) r[k] = fetch(c + k * step);
+        if (__builtin_amdgcn_ballot_w64(c < lo || c + (N - 1) * step >= hi)) {
 #pragma unroll
-        for (int k = 0; k < N; ++k) unpack<CLEAN>(c + k * step, r[k], x[k]);
+            for (int k = 0; k < N; ++k) ends(c + k * step, r[k]);
+        }
+#pragma unroll
+        for (int k = 0; k < N; ++k) unpack<CLEAN>(r[k], x[k]);
     }
 };
 
@@ -231,7 +247,7 @@ __device__ __forceinline__ Found<V> find_prefix(const V* part, int n, int lane, 
 
 // One wavefront per block of 2048 logits, four blocks per workgroup.
 template <bool BF16>
-__global__ void __launch_bounds__(kThreads) k_sample_blocks(const SampleArgs a) {
+__global__ void __launch_bounds__(kThreads, 4) k_sample_blocks(const SampleArgs a) {
     touch_args<SampleArgs>();
     const int lane = threadIdx.x & 63;
     const int row = a.div_wg.div((int)blockIdx.x);
@@ -285,47 +301,75 @@ __global__ void __launch_bounds__(kThreads) k_sample_blocks(const SampleArgs a) 
     if (lane == 0) a.blocks[(int64_t)row * a.n_blocks + blk] = SampleBlock{sum, (double)M};
 }
 
-// ---- within one workgroup of kSampleThreads
-// Exclusive prefix sums over the threads, and the total.
-template <typename V>
-__device__ __forceinline__ V block_scan(V x, V* s_part, int tid, V& total) {
-    const int lane = tid & 63, wave = tid >> 6;
-    const V incl = wave_incl_scan(x);
-    if (lane == 63) s_part[wave] = incl;
-    __syncthreads();
-    V before = 0;
-    total = 0;
+// Exclusive prefix sums and maxima over the threads of a workgroup, with one barrier each: calls alternate between two arrays, so
+// that what a call writes was last read before the barrier of the call in between.  Every thread makes the same calls.
+struct SampleBlockOps {
+    uint64_t (*part)[kSampleWaves];      // LDS, two of them
+    int lane, wave, turn;
+    template <typename V>
+    __device__ __forceinline__ V scan(V x, V& total) {
+        V* p = reinterpret_cast<V*>(part[turn]);
+        turn ^= 1;
+        const V incl = wave_incl_scan(x);
+        if (lane == 63) p[wave] = incl;
+        __syncthreads();
+        V before = 0;
+        total = 0;
 #pragma unroll
-    for (int w = 0; w < kSampleWaves; ++w) {
-        if (w == wave) before = total;
-        total += s_part[w];
+        for (int w = 0; w < kSampleWaves; ++w) {
+            if (w == wave) before = total;
+            total += p[w];
+        }
+        return before + incl - x;
     }
-    __syncthreads();
-    return before + incl - x;
-}
-template <typename V>
-__device__ __forceinline__ V block_max(V x, V* s_part, int tid) {
-    x = wave_max(x);
-    if ((tid & 63) == 0) s_part[tid >> 6] = x;
-    __syncthreads();
-    x = s_part[0];
+    __device__ __forceinline__ int max(int x) {
+        int* p = reinterpret_cast<int*>(part[turn]);
+        turn ^= 1;
+        x = wave_max(x);
+        if (lane == 0) p[wave] = x;
+        __syncthreads();
+        x = p[0];
 #pragma unroll
-    for (int w = 1; w < kSampleWaves; ++w) x = s_part[w] > x ? s_part[w] : x;
-    __syncthreads();
-    return x;
+        for (int w = 1; w < kSampleWaves; ++w) x = p[w] > x ? p[w] : x;
+        return x;
+    }
+};
+
+// body(k, load(k)) for k in [0, n), n <= n_max (n_max uniform, n - 1 >= 0 or nothing), four loads on their way at a time.
+template <typename Load, typename Body>
+__device__ __forceinline__ void each_of(int n, int n_max, Load load, Body body) {
+#pragma unroll 1
+    for (int k0 = 0; k0 < n_max; k0 += 4) {
+        decltype(load(0)) x[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) x[k] = load(max(0, min(k0 + k, n - 1)));
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (k0 + k < n) body(k0 + k, x[k]);
+    }
 }
 
-// Descending over the lanes: a bitonic sort through lane exchanges.
-__device__ __forceinline__ uint64_t wave_sort(uint64_t x, int lane) {
+__device__ __forceinline__ uint64_t read_lane(uint64_t x, int lane) {
+    return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(x >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)x, lane);
+}
+
+// The n <= 64 entries of a list in LDS (all different), in descending order over the lanes (0 behind the last one), by one wavefront: an
+// entry's place is the number of larger ones.  `sorted` is LDS for 64 entries; wavefronts may share it if they order the same list.
+__device__ __forceinline__ uint64_t wave_order(const uint64_t* list, int n, uint64_t* sorted, int lane) {
+    const uint64_t x = lane < n ? list[lane] : ~0ull;
+    int rank = lane < n ? 0 : lane;
+    int j = 0;
+    for (; j + 8 <= n; j += 8) {
+        uint64_t y[8];                   // (all on their way before the first is looked at)
 #pragma unroll
-    for (int run = 2; run <= 64; run *= 2)
+        for (int k = 0; k < 8; ++k) y[k] = list[j + k];
 #pragma unroll
-        for (int gap = run / 2; gap; gap /= 2) {
-            const uint64_t y = __shfl_xor(x, gap);
-            const bool larger = ((lane & gap) == 0) == ((lane & run) == 0);      // this lane keeps the larger one
-            x = (x > y) == larger ? x : y;
-        }
-    return x;
+        for (int k = 0; k < 8; ++k) rank += y[k] > x ? 1 : 0;
+    }
+    for (; j < n; ++j) rank += list[j] > x ? 1 : 0;
+    sorted[rank] = lane < n ? x : 0ull;
+    __builtin_amdgcn_wave_barrier();
+    return sorted[lane];
 }
 
 // A list entry: larger is earlier in the order (logit descending, index ascending).
@@ -333,21 +377,23 @@ __device__ __forceinline__ uint64_t list_entry(uint32_t key, int e) { return (ui
 __device__ __forceinline__ float entry_value(uint64_t x) { return key_value((uint32_t)(x >> 32)); }
 __device__ __forceinline__ int entry_index(uint64_t x) { return (int)(0xffffffffu - (uint32_t)x); }
 
-struct BinFound { int bin, reached; uint32_t before; unsigned long long mass; };      // before, mass: of the bins ahead of it
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ u16x2 halves(uint32_t x) { return __builtin_bit_cast(u16x2, x); }
+
+struct BinFound { int bin, reached; uint32_t before; uint64_t mass; };      // before, mass: of the bins ahead of it
 
 template <bool BF16>
 __global__ void __launch_bounds__(kSampleThreads) k_sample_pick(const SampleArgs a) {
     __shared__ __align__(16) char s_mem[kSampleList * 8];
     __shared__ uint64_t s_sorted[kSampleSort];
-    __shared__ unsigned long long s_mass[kSampleBins], s_above, s_part64[kSampleWaves];
+    __shared__ unsigned long long s_mass[kSampleBins], s_above;
+    __shared__ uint64_t s_part[2][kSampleWaves];
     __shared__ uint32_t s_count[kSampleBins], s_digit;
-    __shared__ double s_part[kSampleWaves];
-    __shared__ int s_int[kSampleWaves];
-    __shared__ BinFound s_bin;
     static_assert(kSampleMaxIters * kSampleWaves * 12 + 256 * 8 <= sizeof(s_mem) && kSampleMaxBlocks * 8 <= sizeof(s_mem), "one array for every way");
     static_assert(sizeof(s_sorted) == kSampleList * 4, "the chunks of the candidates lie where a bin is sorted later");
 
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    SampleBlockOps block{s_part, lane, wave, 0};
     touch_args<SampleArgs>();
     const int row = blockIdx.x, b = a.div_T.div(row), i = row - b * a.T;
     int32_t* const token = a.tokens + row;
@@ -404,49 +450,43 @@ __global__ void __launch_bounds__(kSampleThreads) k_sample_pick(const SampleArgs
         for (int k = lane; k < a.n_blocks; k += 64) {
             const SampleBlock x = blocks[k];
             const double v = x.sum == 0.0 ? 0.0 : x.sum * weight.of_block(x.max);
-            if (wave == 0) s_sum[k] = v;
+            s_sum[k] = v;              // (every wavefront writes what it reads below: the same values)
             total += v;
         }
         total = wave_sum(total);
     }
     if (!rule.filters()) {
-        if (wave) return;
         __builtin_amdgcn_wave_barrier();
         const Found<double> f = find_prefix(s_sum, a.n_blocks, lane, [&](double all) { return (double)u * all; });
         const double target = (double)u * f.total;
         const bool past = u >= 1.f || f.before >= f.total;      // nothing exceeds the target: the last positive weight
-        double w[32], sum = 0.0;
-        float x[4][8];
-        logits.load_each(f.at * kSampleChunks + lane * 4, 1, x);
+        constexpr int PER = kSampleBlock / kSampleThreads;      // logits of a thread
+        static_assert(PER == 4);
+        float x[8];
+        const int c = f.at * kSampleChunks + tid / 2, e0 = logits.first(c) + PER * (tid & 1);
+        logits.load(c, x);
+        double w[PER], sum = 0.0, all;
 #pragma unroll
-        for (int j = 0; j < 32; ++j) {
-            w[j] = weight(x[j >> 3][j & 7]);
+        for (int j = 0; j < PER; ++j) {
+            w[j] = weight(tid & 1 ? x[PER + j] : x[j]);
             sum += w[j];
         }
-        const int e0 = logits.first(f.at * kSampleChunks + lane * 4);
-        double run = f.before + wave_incl_scan(sum) - sum, wf = 0.0;
+        double run = f.before + block.scan(sum, all), wf = 0.0;
         int found = -1, last = -1;
 #pragma unroll
-        for (int j = 0; j < 32; ++j) {
+        for (int j = 0; j < PER; ++j) {
             run += w[j];
-            if (w[j] > 0.0) {
-                if (found < 0) wf = w[j];
+            if (w[j] > 0.0 && found < 0) {
+                wf = w[j];
                 last = e0 + j;
-                if (found < 0 && run > target) found = last;
+                if (!past && run > target) found = last;
             }
         }
-        const uint64_t hit = past ? 0ull : __builtin_amdgcn_ballot_w64(found >= 0);
-        const uint64_t some = __builtin_amdgcn_ballot_w64(last >= 0);
-        const int who = hit ? (int)__builtin_ctzll(hit) : 63 - (int)__builtin_clzll(some | 1ull);
-        if (lane == who) {
-            if (!hit) {
-#pragma unroll
-                for (int j = 0; j < 32; ++j)
-                    if (w[j] > 0.0) wf = w[j];
-            }
-            *token = hit ? found : last;
-            if (prob) *prob = (float)(wf / f.total);
-        }
+        // the first thread with an element beyond the target, or else the last one with a weight
+        const int claim = found >= 0 ? 0x40000000 - tid : (last >= 0 ? tid - 0x40000000 : -0x7fffffff);
+        if (block.max(claim) != claim || last < 0) return;
+        *token = last;
+        if (prob) *prob = (float)(wf / f.total);
         return;
     }
 
@@ -454,81 +494,72 @@ __global__ void __launch_bounds__(kSampleThreads) k_sample_pick(const SampleArgs
     const uint16_t* maxima = a.maxima + (int64_t)row * a.n_blocks * kSampleChunks;
     const int n_groups8 = a.n_blocks * (kSampleChunks / 8);
     const int n_it = (n_groups8 + kSampleThreads - 1) / kSampleThreads;
-    // body(iteration, first of this thread's eight chunks, their eight halves); chunks are in index order over (iteration, thread).  The
-    // first HELD iterations' (vocabularies of up to 262144) are fetched once and stay in registers.
-    constexpr int HELD = 8;
-    auto fetch_max = [&](int it) { return *reinterpret_cast<const u32x4*>(maxima + 8 * min(it * kSampleThreads + tid, n_groups8 - 1)); };
-    u32x4 held[HELD];
-#pragma unroll
-    for (int k = 0; k < HELD; ++k) {
-        if (k >= n_it) break;             // (uniform)
-        held[k] = fetch_max(k);
-    }
+    // A thread has n_it consecutive groups of eight chunks, in order; eight groups at a time: body(first chunk, four pairs of halves each).
+    auto fetch_max = [&](int it) { return *reinterpret_cast<const u32x4*>(maxima + 8 * min(tid * n_it + it, n_groups8 - 1)); };
     auto each_max = [&](auto&& body) {
-        auto one = [&](int it, u32x4 x) {
-            const int g = it * kSampleThreads + tid;
-            body(it, 8 * g, g < n_groups8 ? x : u32x4{0, 0, 0, 0});
-        };
+#pragma unroll 1
+        for (int it0 = 0; it0 < n_it; it0 += 8) {
+            u32x4 x[8];
 #pragma unroll
-        for (int k = 0; k < HELD; ++k) {
-            if (k >= n_it) break;
-            one(k, held[k]);
-        }
-        for (int it0 = HELD; it0 < n_it; it0 += 4) {
-            u32x4 x[4];
+            for (int k = 0; k < 8; ++k) x[k] = it0 + k < n_it ? fetch_max(it0 + k) : u32x4{0, 0, 0, 0};
 #pragma unroll
-            for (int k = 0; k < 4; ++k) x[k] = fetch_max(it0 + k);
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-                if (it0 + k < n_it) one(it0 + k, x[k]);
+            for (int k = 0; k < 8; ++k)
+                if (it0 + k >= n_it || tid * n_it + it0 + k >= n_groups8) x[k] = u32x4{0, 0, 0, 0};
+            body(8 * (tid * n_it + it0), x);
         }
     };
-    auto mass = [&](uint32_t k) { return (unsigned long long)(weight(key_value(k)) * a.mass_scale + 0.5); };
-    auto clear_bins = [&] {
+    auto each_half = [&](auto&& body) {      // one by one (where the code's length counts more)
+#pragma unroll 1
+        for (int it = 0; it < n_it; ++it) {
+            u32x4 x = tid * n_it + it < n_groups8 ? fetch_max(it) : u32x4{0, 0, 0, 0};
+#pragma unroll 1
+            for (int j = 0; j < 8; ++j) {
+                body(x[0] & 0xffffu);
+                x = u32x4{__builtin_amdgcn_alignbit(x[1], x[0], 16), __builtin_amdgcn_alignbit(x[2], x[1], 16), __builtin_amdgcn_alignbit(x[3], x[2], 16), x[3] >> 16};
+            }
+        }
+    };
+    auto mass = [&](uint32_t k) { return (uint64_t)(weight(key_value(k)) * a.mass_scale + 0.5); };
+    auto clear_bins = [&] {              // (a barrier follows before they are used)
         if (tid < kSampleBins) {
             s_mass[tid] = 0;
             s_count[tid] = 0;
         }
-        __syncthreads();
     };
-    // The first bin up to which the entries number `n` or more, or weigh `m` or more (the last one that holds any, if none does).
+    clear_bins();
+    // The first bin up to which the entries number `n` or more, or weigh `m` or more (the last one that holds any, if none does).  By every
+    // wavefront for itself.
     auto find_bin = [&](bool by_mass, uint32_t n, double m) {
-        __syncthreads();
-        if (wave == 0) {
-            constexpr int PER = kSampleBins / 64;
-            uint32_t c[PER], cs = 0;
-            unsigned long long w[PER], ws = 0;
+        constexpr int PER = kSampleBins / 64;
+        uint32_t c[PER], cs = 0;
+        uint64_t w[PER], ws = 0;
 #pragma unroll
-            for (int j = 0; j < PER; ++j) {
-                c[j] = s_count[PER * lane + j];
-                w[j] = s_mass[PER * lane + j];
-                cs += c[j];
-                ws += w[j];
-            }
-            const uint32_t ci = wave_incl_scan(cs);
-            const unsigned long long wi = wave_incl_scan(ws);
-            const uint64_t reached = __builtin_amdgcn_ballot_w64(cs > 0 && (by_mass ? (double)wi >= m : ci >= n));
-            const uint64_t some = __builtin_amdgcn_ballot_w64(cs > 0);
-            const int who = reached ? (int)__builtin_ctzll(reached) : 63 - (int)__builtin_clzll(some | 1ull);
-            if (lane == who) {
-                BinFound f{0, reached != 0, 0u, 0ull};
-                uint32_t run = ci - cs;
-                unsigned long long weigh = wi - ws;
-#pragma unroll
-                for (int j = 0; j < PER; ++j) {
-                    if (c[j] == 0 || (f.reached == 2)) continue;
-                    f.bin = PER * lane + j;
-                    f.before = run;
-                    f.mass = weigh;
-                    run += c[j];
-                    weigh += w[j];
-                    if (reached && (by_mass ? (double)weigh >= m : run >= n)) f.reached = 2;
-                }
-                s_bin = f;
-            }
+        for (int j = 0; j < PER; ++j) {
+            c[j] = s_count[PER * lane + j];
+            w[j] = s_mass[PER * lane + j];
+            cs += c[j];
+            ws += w[j];
         }
-        __syncthreads();
-        return s_bin;
+        const uint32_t ci = wave_incl_scan(cs);
+        const uint64_t wi = wave_incl_scan(ws);
+        const uint64_t reached = __builtin_amdgcn_ballot_w64(cs > 0 && (by_mass ? (double)wi >= m : ci >= n));
+        const uint64_t some = __builtin_amdgcn_ballot_w64(cs > 0);
+        const int who = reached ? (int)__builtin_ctzll(reached) : 63 - (int)__builtin_clzll(some | 1ull);
+        BinFound f{0, 0, 0u, 0ull};      // (of this lane's bins; that of lane `who` counts)
+        uint32_t run = ci - cs;
+        uint64_t weigh = wi - ws;
+        bool done = false;
+#pragma unroll
+        for (int j = 0; j < PER; ++j) {
+            if (c[j] == 0 || done) continue;
+            f.bin = PER * lane + j;
+            f.before = run;
+            f.mass = weigh;
+            run += c[j];
+            weigh += w[j];
+            done = by_mass ? (double)weigh >= m : run >= n;
+        }
+        return BinFound{__builtin_amdgcn_readlane(f.bin, who), reached != 0, (uint32_t)__builtin_amdgcn_readlane((int)f.before, who), read_lane(f.mass, who)};
     };
     uint32_t tau_m = 0;                      // min-p's threshold
     if (rule.by_m) {
@@ -553,11 +584,16 @@ __global__ void __launch_bounds__(kSampleThreads) k_sample_pick(const SampleArgs
     if (rule.by_k) {
         // the k-th largest of the maxima of groups of chunks, four per thread (the lower edge of its bin): as many logits are as large.  With
         // fewer groups the least of the maxima of all chunks, if there are k.
-        uint32_t v[4] = {0, 0, 0, 0};
-        each_max([&](int, int, u32x4 x) {
+        u16x2 v2[4] = {};
+        each_max([&](int, const u32x4 (&x)[8]) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) v[j] = max(v[j], max(x[j] & 0xffffu, x[j] >> 16));
+            for (int k = 0; k < 8; ++k)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v2[j] = __builtin_elementwise_max(v2[j], halves(x[k][j]));
         });
+        uint32_t v[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = max((uint32_t)v2[j][0], (uint32_t)v2[j][1]);
         int count = 0, n_held;
         uint32_t least = 0xffffu;
 #pragma unroll
@@ -566,29 +602,25 @@ __global__ void __launch_bounds__(kSampleThreads) k_sample_pick(const SampleArgs
                 ++count;
                 least = min(least, v[j]);
             }
-        block_scan(count, s_int, tid, n_held);
+        block.scan(count, n_held);
         const bool by_groups = n_held >= rule.top_k;
         if (!by_groups) {
             count = 0;
             least = 0xffffu;
-            each_max([&](int, int, u32x4 x) {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const uint32_t half = j & 1 ? x[j >> 1] >> 16 : x[j >> 1] & 0xffffu;
-                    count += half >= lowest >> 16 ? 1 : 0;
-                    least = half >= lowest >> 16 ? min(least, half) : least;
-                }
+            each_half([&](uint32_t half) {
+                count += half >= lowest >> 16 ? 1 : 0;
+                least = half >= lowest >> 16 ? min(least, half) : least;
             });
-            block_scan(count, s_int, tid, n_held);
+            block.scan(count, n_held);
         }
         if (n_held >= rule.top_k) {
-            uint32_t edge = (uint32_t)(0xffff - block_max((int)(0xffffu - least), s_int, tid));
+            uint32_t edge = (uint32_t)(0xffff - block.max((int)(0xffffu - least)));
             if (by_groups) {
                 const int shift = bin_shift(top_half - edge);
-                clear_bins();
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
                     if (v[j] >= edge) atomicAdd(&s_count[(top_half - v[j]) >> shift], 1u);
+                __syncthreads();
                 edge = max(edge, bin_edge(find_bin(false, (uint32_t)rule.top_k, 0.0), shift));
             }
             lo = edge << 16;
@@ -605,134 +637,116 @@ __global__ void __launch_bounds__(kSampleThreads) k_sample_pick(const SampleArgs
     // ---- the candidates, in index order.  First chunks whose maximum (its upper half's upper end) reaches a bound, then their logits.
     uint64_t* s_list = reinterpret_cast<uint64_t*>(s_mem);
     uint32_t* s_chunk = reinterpret_cast<uint32_t*>(s_sorted);
-    // how many chunks' halves reach `half`; (half, chunk) of each to s_list if they fit
-    auto list_chunks = [&](uint32_t half) {
-        // counts by (iteration, wavefront), their prefix sums, then the places
-        uint32_t* s_hits = s_chunk;
-        auto hits_of = [&](u32x4 x) {            // of eight chunks
-            uint32_t hits = 0;
+    // how many chunks' halves reach `half`; the chunks to `list` if they fit
+    auto list_chunks = [&](uint32_t half, uint32_t* list) {
+        const uint32_t less = half - 1;          // (half is 0x80 or more: that of the lowest finite key)
+        auto hits_of = [&](const u32x4 (&x)[8]) {
+            uint64_t hits = 0;                   // bit 8 k + j: chunk j of group k
 #pragma unroll
-            for (int j = 0; j < 4; ++j) hits |= ((x[j] & 0xffffu) >= half ? 1u : 0u) << (2 * j) | ((x[j] >> 16) >= half ? 2u : 0u) << (2 * j);
+            for (int k = 0; k < 8; ++k) {
+                uint32_t two = 0;                // bits 0, 2, 4, 6: the lower halves, 16, 18, ..: the upper ones
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const u16x2 over = __builtin_elementwise_sub_sat(halves(x[k][j]), u16x2{(uint16_t)less, (uint16_t)less});
+                    two |= __builtin_bit_cast(uint32_t, __builtin_elementwise_min(over, u16x2{1, 1})) << (2 * j);
+                }
+                hits |= (uint64_t)((two | two >> 15) & 0xffu) << (8 * k);
+            }
             return hits;
         };
-        auto count_before = [&](uint32_t hits, int& all) {      // hits of the wavefront's lanes before this one, and of all
-            const uint32_t c = (uint32_t)__builtin_popcount(hits);
-            int before = 0;
-            all = 0;
-#pragma unroll
-            for (int bit = 0; bit < 4; ++bit) {
-                const uint64_t m = __builtin_amdgcn_ballot_w64(c >> bit & 1u);
-                before += (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0u)) << bit;
-                all += __builtin_popcountll(m) << bit;
+        int mine = 0, n_hit;
+        uint64_t hits;
+        each_max([&](int, const u32x4 (&x)[8]) { mine += __builtin_popcountll(hits = hits_of(x)); });
+        int to = block.scan(mine, n_hit);
+        clear_bins();
+        if (n_hit <= kSampleList) {
+            auto put = [&](int c) {
+                for (; hits; hits &= hits - 1) list[to++] = (uint32_t)(c + __builtin_ctzll(hits));
+            };
+            if (n_it <= 8) {
+                put(8 * tid * n_it);
+            } else {
+                each_max([&](int c, const u32x4 (&x)[8]) {
+                    hits = hits_of(x);
+                    put(c);
+                });
             }
-            return before;
-        };
-        int n_hit, all;
-        __syncthreads();
-        each_max([&](int it, int, u32x4 x) {
-            count_before(hits_of(x), all);
-            if (lane == 0) s_hits[it * kSampleWaves + wave] = (uint32_t)all;
-        });
-        __syncthreads();
-        const int per = (n_it * kSampleWaves + kSampleThreads - 1) / kSampleThreads;
-        int sum = 0;
-        for (int k = tid * per; k < min(n_it * kSampleWaves, (tid + 1) * per); ++k) sum += (int)s_hits[k];
-        int at = block_scan(sum, s_int, tid, n_hit);
-        if (n_hit > kSampleList) return n_hit;
-        for (int k = tid * per; k < min(n_it * kSampleWaves, (tid + 1) * per); ++k) {
-            const int c = (int)s_hits[k];
-            s_hits[k] = (uint32_t)at;
-            at += c;
         }
-        __syncthreads();
-        each_max([&](int it, int c, u32x4 x) {
-            const uint32_t hits = hits_of(x);
-            int to = (int)s_hits[it * kSampleWaves + wave] + count_before(hits, all);
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-                if (hits >> j & 1u) s_list[to++] = (uint64_t)(j & 1 ? x[j >> 1] >> 16 : x[j >> 1] & 0xffffu) << 32 | (uint32_t)(c + j);
-        });
         __syncthreads();
         return n_hit;
     };
     // Of these, by bins of equal width in halves: where the chunks' maxima alone (their lower ends) suffice, nothing beyond that bin is
     // kept.  (By count the bound is as good already, unless the list is too long.)
     uint32_t half = lo >> 16;
-    int n_hit = list_chunks(half);
-    if (n_hit > kSampleList ? rule.by_k || rule.by_p : rule.by_p && !rule.by_k) {
+    const bool by_mass = rule.by_p && !rule.by_k;
+    uint32_t* s_first = by_mass ? reinterpret_cast<uint32_t*>(s_mem) : s_chunk;
+    uint16_t* s_half = reinterpret_cast<uint16_t*>(s_mem + kSampleList * 4);
+    int n_hit = list_chunks(half, s_first);
+    if (by_mass || (rule.by_k && n_hit > kSampleList)) {
         const int shift = bin_shift(top_half - half);
-        clear_bins();
         auto count = [&](uint32_t h) {
             if (h << 16 < lo) return;
             const uint32_t at = (top_half - h) >> shift;
             atomicAdd(&s_count[at], 1u);
-            if (!rule.by_k) atomicAdd(&s_mass[at], mass(h << 16));
+            if (by_mass) atomicAdd(&s_mass[at], mass(h << 16));
         };
-        if (n_hit <= kSampleList) {
-            for (int l = tid; l < n_hit; l += kSampleThreads) count((uint32_t)(s_list[l] >> 32));
+        const bool fits = n_hit <= kSampleList;
+        const int q = (n_hit + kSampleThreads - 1) / kSampleThreads, h0 = min(n_hit, tid * q), h1 = min(n_hit, h0 + q);
+        if (fits) {
+            each_of(h1 - h0, q, [&](int k) { return maxima[s_first[min(h0 + k, n_hit - 1)]]; },
+                    [&](int k, uint16_t h) {
+                        s_half[h0 + k] = h;
+                        count(h);
+                    });
         } else {
-            each_max([&](int, int, u32x4 x) {
-#pragma unroll 1
-                for (int j = 0; j < 8; ++j) {
-                    count(x[0] & 0xffffu);
-                    x = u32x4{__builtin_amdgcn_alignbit(x[1], x[0], 16), __builtin_amdgcn_alignbit(x[2], x[1], 16), __builtin_amdgcn_alignbit(x[3], x[2], 16), x[3] >> 16};
-                }
-            });
+            each_half(count);
         }
-        half = max(half, bin_edge(find_bin(!rule.by_k, (uint32_t)rule.top_k, (double)rule.top_p * (1.0 + 1e-9) * total * a.mass_scale), shift));
+        __syncthreads();
+        half = max(half, bin_edge(find_bin(by_mass, (uint32_t)rule.top_k, (double)rule.top_p * (1.0 + 1e-9) * total * a.mass_scale), shift));
         lo = max(lo, half << 16);
+        if (fits) {
+            int mine = 0;
+            for (int h = h0; h < h1; ++h) mine += s_half[h] >= half ? 1 : 0;
+            int at = block.scan(mine, n_hit);
+            clear_bins();
+            for (int h = h0; h < h1; ++h)
+                if (s_half[h] >= half) s_chunk[at++] = s_first[h];
+            __syncthreads();
+        } else {
+            n_hit = list_chunks(half, s_chunk);
+        }
     }
-    if (n_hit > kSampleList) n_hit = list_chunks(half);
     bool listed = n_hit <= kSampleList;
     int n = 0;
     if (listed) {
-        // those that remain, to s_chunk
-        int q = (n_hit + kSampleThreads - 1) / kSampleThreads, h0 = min(n_hit, tid * q), h1 = min(n_hit, h0 + q), mine = 0;
-        for (int h = h0; h < h1; ++h) mine += (uint32_t)(s_list[h] >> 32) >= half ? 1 : 0;
-        int all, at = block_scan(mine, s_int, tid, all);
-        for (int h = h0; h < h1; ++h)
-            if ((uint32_t)(s_list[h] >> 32) >= half) s_chunk[at++] = (uint32_t)s_list[h];
-        n_hit = all;
-        __syncthreads();
-        // their logits: up to eight chunks of a thread stay in registers between counting and listing
-        constexpr int HOLD = 8;
-        q = (n_hit + kSampleThreads - 1) / kSampleThreads;
-        h0 = min(n_hit, tid * q);
-        h1 = min(n_hit, h0 + q);
-        typename SampleRow<BF16>::Raw raw[HOLD];
-        int c[HOLD];
+        // their logits, a chunk per thread at a time
+        typename SampleRow<BF16>::Raw raw = {};
+        int c = -1;
         auto fetch = [&](int h) {
-#pragma unroll
-            for (int k = 0; k < HOLD; ++k) {
-                if (k >= q) break;         // (uniform)
-                c[k] = h + k < h1 ? (int)s_chunk[h + k] : -1;
-                raw[k] = logits.fetch(c[k]);
-            }
+            c = h < n_hit ? (int)s_chunk[h] : -1;
+            raw = logits.fetch(c);
         };
-        auto each_logit = [&](auto&& body) {
+        fetch(tid);
+#pragma unroll 1
+        for (int h = tid; h - tid < n_hit; h += kSampleThreads) {
+            float x[8];
+            const int e0 = logits.first(c);
+            uint32_t hits = 0;
+            if (c >= 0) {
+                logits.ends(c, raw);
+                logits.unpack(raw, x);
 #pragma unroll
-            for (int k = 0; k < HOLD; ++k) {
-                if (k >= q) break;
-                if (c[k] < 0) continue;
-                float x[8];
-                logits.unpack(c[k], raw[k], x);
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    if (order_key(x[j]) >= lo) body(order_key(x[j]), logits.first(c[k]) + j);
+                for (int j = 0; j < 8; ++j) hits |= (order_key(x[j]) >= lo ? 1u : 0u) << j;
             }
-        };
-        mine = 0;
-        for (int h = h0; h < h1; h += HOLD) {
-            fetch(h);
-            each_logit([&](uint32_t, int) { ++mine; });
+            fetch(h + kSampleThreads);
+            int all, at = n + block.scan(__builtin_popcount(hits), all);
+            n += all;
+            if (n > kSampleList) break;
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (hits >> j & 1u) s_list[at++] = list_entry(order_key(x[j]), e0 + j);
         }
-        at = block_scan(mine, s_int, tid, n);
         listed = n <= kSampleList;
-        if (listed)
-            for (int h = h0; h < h1; h += HOLD) {
-                if (q > HOLD) fetch(h);
-                each_logit([&](uint32_t key, int e) { s_list[at++] = list_entry(key, e); });
-            }
         __syncthreads();
     }
 
@@ -746,7 +760,7 @@ __global__ void __launch_bounds__(kSampleThreads) k_sample_pick(const SampleArgs
         const uint64_t entry = lane < n ? s_list[lane] : 0ull;
         uint64_t last_kept = 0;
         if (rule.by_k || rule.by_p) {
-            const uint64_t x = wave_sort(entry, lane);
+            const uint64_t x = wave_order(s_list, n, s_sorted, lane);
             int kept = rule.by_k ? min(rule.top_k, n) : n;
             if (rule.by_p) {
                 const double cum = wave_incl_scan(lane < n ? weight(entry_value(x)) : 0.0);
@@ -766,33 +780,35 @@ __global__ void __launch_bounds__(kSampleThreads) k_sample_pick(const SampleArgs
         return;
     }
     const int q = (n + kSampleThreads - 1) / kSampleThreads, l0 = min(n, tid * q), l1 = min(n, l0 + q);     // this thread's entries
+    auto entry = [&](int k) { return s_list[l0 + k]; };
     uint64_t last_kept = 0;             // the last entry that is kept
     if (listed && (rule.by_k || rule.by_p)) {
         // ---- the exact threshold: a histogram of the list, and the entries of the bin in which it falls in order
-        clear_bins();
-        for (int l = l0; l < l1; ++l) {
-            const uint32_t key = (uint32_t)(s_list[l] >> 32);
-            const int at = bin_of(key_value(key));
+        each_of(l1 - l0, q, entry, [&](int, uint64_t x) {
+            const int at = bin_of(entry_value(x));
             atomicAdd(&s_count[at], 1u);
-            if (rule.by_p) atomicAdd(&s_mass[at], mass(key));
-        }
-        // the entries of a bin into s_sorted, descending; how many
-        auto sort_bin = [&](int bin) {
-            int mine = 0, m;
-            for (int l = l0; l < l1; ++l) mine += bin_of(entry_value(s_list[l])) == bin ? 1 : 0;
-            int at = block_scan(mine, s_int, tid, m);
+            if (rule.by_p) atomicAdd(&s_mass[at], mass((uint32_t)(x >> 32)));
+        });
+        __syncthreads();
+        // The entries of a bin in order, and how many there are: up to 64 (as a rule there are ten to forty) with the lanes of every wavefront, and
+        // their running mass; more in LDS.
+        uint64_t x = 0, x_run = 0;
+        auto order_bin = [&](int bin) {
+            uint32_t mine = 0;                   // which of this thread's entries (at most eight)
+            each_of(l1 - l0, q, entry, [&](int k, uint64_t x) { mine |= (bin_of(entry_value(x)) == bin ? 1u : 0u) << k; });
+            int m, at = block.scan(__builtin_popcount(mine), m);
             if (m > kSampleSort) return m;
-            for (int l = l0; l < l1; ++l)
-                if (bin_of(entry_value(s_list[l])) == bin) s_sorted[at++] = s_list[l];
-            int size = 64;
+            for (; mine; mine &= mine - 1) s_sorted[at++] = s_list[l0 + __builtin_ctz(mine)];
+            if (m <= 64) {
+                __syncthreads();
+                x = wave_order(s_sorted, m, s_sorted + 64, lane);
+                x_run = rule.by_p ? wave_incl_scan(lane < m ? mass((uint32_t)(x >> 32)) : 0ull) : 0ull;
+                return m;
+            }
+            int size = 128;
             while (size < m) size *= 2;
             for (int k = m + tid; k < size; k += kSampleThreads) s_sorted[k] = 0ull;
             __syncthreads();
-            if (size == 64) {              // one wavefront, by lane exchanges
-                if (wave == 0) s_sorted[lane] = wave_sort(s_sorted[lane], lane);
-                __syncthreads();
-                return m;
-            }
             for (int run = 2; run <= size; run *= 2)
                 for (int gap = run / 2; gap; gap /= 2) {
                     for (int k = tid; k < size / 2; k += kSampleThreads) {
@@ -807,61 +823,65 @@ __global__ void __launch_bounds__(kSampleThreads) k_sample_pick(const SampleArgs
                 }
             return m;
         };
-        // of the first m sorted entries: how many come before the running mass from `base` reaches the target; their whole mass
-        auto reach_mass = [&](int m, unsigned long long base, double target, unsigned long long& all) {
-            const int s = (m + kSampleThreads - 1) / kSampleThreads, k0 = min(m, tid * s), k1 = min(m, k0 + s);
-            unsigned long long sum = 0;
+        auto nth = [&](int m, int n) { return m <= 64 ? read_lane(x, n) : s_sorted[n]; };
+        // of the first r of m ordered entries: their mass; how many come before the running mass from `base` reaches the target
+        auto sum_of = [&](int k0, int k1) {
+            uint64_t sum = 0;
             for (int k = k0; k < k1; ++k) sum += mass((uint32_t)(s_sorted[k] >> 32));
-            unsigned long long run = base + block_scan(sum, s_part64, tid, all);
+            return sum;
+        };
+        auto mass_of_first = [&](int m, int r) {
+            if (m <= 64) return read_lane(x_run, r - 1);
+            const int s = (r + kSampleThreads - 1) / kSampleThreads;
+            uint64_t all;
+            block.scan(sum_of(min(r, tid * s), min(r, (tid + 1) * s)), all);
+            return all;
+        };
+        auto reach_mass = [&](int m, int r, uint64_t base, double target) {
+            if (m <= 64) return (int)__builtin_popcountll(__builtin_amdgcn_ballot_w64(lane < r && (double)(base + x_run) < target));
+            const int s = (r + kSampleThreads - 1) / kSampleThreads, k0 = min(r, tid * s), k1 = min(r, k0 + s);
+            uint64_t all, run = base + block.scan(sum_of(k0, k1), all);
             int below = 0, n_below;
             for (int k = k0; k < k1; ++k) {
                 run += mass((uint32_t)(s_sorted[k] >> 32));
                 below += (double)run < target ? 1 : 0;
             }
-            block_scan(below, s_int, tid, n_below);
+            block.scan(below, n_below);
             return n_below;
         };
+        // by count, then by mass if that ends in another bin, or by mass alone
         double target = (double)rule.top_p * total * a.mass_scale;
-        bool done = false;
-        if (rule.by_k) {
-            const BinFound f = find_bin(false, (uint32_t)rule.top_k, 0.0);
-            const int m = sort_bin(f.bin);
+        bool of_mass = !rule.by_k;
+#pragma unroll 1
+        for (;;) {
+            const BinFound f = find_bin(of_mass, (uint32_t)rule.top_k, target);
+            const int m = order_bin(f.bin);
             listed = m <= kSampleSort;
-            if (listed) {
-                const int r = max(1, min(m, rule.top_k - (int)f.before));       // the k-th entry is the r-th of the bin (all, if there are fewer than k)
-                last_kept = s_sorted[r - 1];
-                if (rule.by_p) {
-                    unsigned long long all;
-                    reach_mass(r, 0ull, 0.0, all);
-                    target = (double)rule.top_p * (double)(f.mass + all);
-                    if ((double)f.mass < target) {
-                        last_kept = s_sorted[min(reach_mass(r, f.mass, target, all), r - 1)];
-                        done = true;
-                    }
-                }
+            if (!listed) break;
+            int r = m;
+            if (!of_mass) {
+                r = max(1, min(m, rule.top_k - (int)f.before));       // the k-th entry is the r-th of the bin (all, if there are fewer than k)
+                last_kept = nth(m, r - 1);
+                if (!rule.by_p) break;
+                target = (double)rule.top_p * (double)(f.mass + mass_of_first(m, r));
+                of_mass = (double)f.mass >= target;
+                if (of_mass) continue;
             }
-        }
-        if (rule.by_p && listed && !done) {
-            const BinFound f = find_bin(true, 0u, target);
-            const int m = sort_bin(f.bin);
-            listed = m <= kSampleSort;
-            if (listed) {
-                unsigned long long all;
-                last_kept = s_sorted[max(0, min(reach_mass(m, f.mass, target, all), m - 1))];
-            }
+            last_kept = nth(m, max(0, min(reach_mass(m, r, f.mass, target), r - 1)));
+            break;
         }
     }
     if (listed) {
         // ---- the kept entries in index order: the one whose running sum passes u
         auto kept_weight = [&](uint64_t x) { return x >= last_kept && (uint32_t)(x >> 32) >= tau_m ? weight(entry_value(x)) : 0.0; };
         double sum = 0.0, all;
-        for (int l = l0; l < l1; ++l) sum += kept_weight(s_list[l]);
-        const double before = block_scan(sum, s_part, tid, all);
+        each_of(l1 - l0, q, entry, [&](int, uint64_t x) { sum += kept_weight(x); });
+        const double before = block.scan(sum, all);
         const double target = (double)u * all;
         // the first thread that passes the target, or else the last one with a weight
         const bool over = sum > 0.0 && before + sum > target && u < 1.f;
         const int claim = over ? 0x40000000 - tid : (sum > 0.0 ? tid - 0x40000000 : -0x7fffffff);
-        if (block_max(claim, s_int, tid) != claim || !(sum > 0.0)) return;
+        if (block.max(claim) != claim || !(sum > 0.0)) return;
         double run = before, wf = 0.0;
         int at = 0;
         for (int l = l0; l < l1; ++l) {
