@@ -271,7 +271,7 @@ __device__ __forceinline__ void prefix_keys(const PrefixArgs& a, int wg, char* s
 #pragma unroll
         for (int j = 0; j < CW; ++j) acc[rb][j] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    const float raise = kPrefixRaiseLog2 / a.scale_log2;
+    const float raise = fminf(kPrefixRaiseLog2 / a.scale_log2, 3e38f);      // (finite: -inf + raise stays below every score)
     const int full = OWN ? w.len : w.n_keys;       // keys that every row sees
 
     int t = t0 + wave;

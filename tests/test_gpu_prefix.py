@@ -276,3 +276,19 @@ def test_fuzz_of_small_problems():
                         P=top, S=top, strided=bool(rng.random() < 0.3))
         call(args)
         check(args, h)
+
+
+@pytest.mark.parametrize("shape", ["bf16_64", "f32_64"])
+def test_smallest_scale_weighs_all_rows_alike(shape):
+    args, h = setup(40, shape, B=2, T=3, H=16, Hk=1, G=1, plens=[300], lens=[50, 0], scale=2.0 ** -100)
+    call(args)
+    check(args, h)
+
+
+@pytest.mark.parametrize("shape", ["bf16_128", "f32_64"])
+@pytest.mark.parametrize("B, T", [(1, 1), (3, 9), (70, 1)])
+def test_bounds_far_above_the_lengths(shape, B, T):
+    """Slices are planned for the bounds; most of them get nothing."""
+    args, h = setup(41, shape, B=B, T=T, H=4, Hk=1, G=1, plens=[129], lens=[(7 * b) % 90 for b in range(B)], P=60000, S=4000)
+    call(args)
+    check(args, h)

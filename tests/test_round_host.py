@@ -227,3 +227,9 @@ def test_commit_refuses_caches_at_one_place(at):
     good = (25600, 12800, 6400, 64)
     test_commit_refusals(dict(k_stride=good[:at] + (0,) + good[at + 1:]), B.SSV_EINVAL)
     test_commit_refusals(dict(v_stride=good[:at] + (0,) + good[at + 1:]), B.SSV_EINVAL)
+
+
+def test_prefix_refuses_scales_below_2_to_the_minus_100():
+    assert B.ssv_prefix_workspace_bytes(prefix_params(scale=2.0 ** -100)) > 0
+    test_prefix_refusals(dict(scale=2.0 ** -101), B.SSV_EUNSUPPORTED)
+    test_prefix_refusals(dict(scale=1e-40), B.SSV_EUNSUPPORTED)
