@@ -227,16 +227,19 @@ struct RowTileRegs {
 //      and every read is served in two passes; measured on the device);
 //   2: the 64-byte chunk index c / 4 XORed with r & 3 (rows of four chunks) or (r >> 1) & 1 (rows of two): for the
 //      transposing 8-byte reads of a 32x32x16 A operand, in which each half of the wavefront takes 64 bytes of four
-//      consecutive rows (measured: as fast as a linear read; with an unswizzled 256-byte pitch three times slower).
+//      consecutive rows (measured: as fast as a linear read; with an unswizzled 256-byte pitch three times slower);
+//   3: (c & ~15) | ((c & 15) ^ (r & 15)): the reads of policy 1 at a 256-byte pitch, where every row starts at the same bank and sixteen
+//      rows need all sixteen granules (with policy 1 rows 2 i and 2 i + 1 meet: a third more LDS cycles).
 // Rows beyond valid_rows repeat the last valid row (the caller masks their scores; nothing is zero-filled).
 // NT: threads of the workgroup that share the tile's loads.
 template <int ROW_BYTES, int SWZ = 0, int NT = kThreads>
 struct DirectRowTile {
     static constexpr int CPR = ROW_BYTES / 16;            // granules per row
-    static_assert(SWZ == 2 ? (CPR == 8 || CPR == 16) : CPR % 8 == 0, "row length not covered by the swizzle");
+    static_assert(SWZ == 2 ? (CPR == 8 || CPR == 16) : CPR % (SWZ == 3 ? 16 : 8) == 0, "row length not covered by the swizzle");
     __host__ __device__ __forceinline__ static constexpr int swizzled(int r, int c) {
         if constexpr (SWZ == 0) return (c & ~7) | ((c & 7) ^ (r & 7));
         else if constexpr (SWZ == 1) return (c & ~7) | ((c & 7) ^ ((r >> 1) & 7));
+        else if constexpr (SWZ == 3) return (c & ~15) | ((c & 15) ^ (r & 15));
         else return (((c >> 2) ^ (CPR == 16 ? (r & 3) : ((r >> 1) & 1))) << 2) | (c & 3);
     }
     static constexpr int TOTAL = kTile * CPR;

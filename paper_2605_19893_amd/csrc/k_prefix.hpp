@@ -431,7 +431,8 @@ struct PrefixRowsCfg {
 template <int DK, int DV, bool OWN>
 __device__ __forceinline__ void prefix_rows(const PrefixArgs& a, int wg, char* smem, PrefixTree& tree) {
     using Cfg = PrefixRowsCfg<DK, DV>;
-    using KLoader = DirectRowTile<Cfg::KROW, 1, kPrefixThreads>;
+    constexpr int KQ = Cfg::KROW == 256 ? 8 : 4;      // contraction steps after which the swizzle of a K row repeats
+    using KLoader = DirectRowTile<Cfg::KROW, KQ == 8 ? 3 : 1, kPrefixThreads>;
     using VLoader = DirectRowTile<Cfg::VROW, 2, kPrefixThreads>;
     constexpr int STEPS = Cfg::STEPS, MB = Cfg::MB, KT = Cfg::KT, KROW = Cfg::KROW, VROW = Cfg::VROW, STAGE = Cfg::STAGE;
     constexpr int KI = KLoader::ITERS, VI = VLoader::ITERS;     // load instructions per wavefront and tile
@@ -495,12 +496,12 @@ __device__ __forceinline__ void prefix_rows(const PrefixArgs& a, int wg, char* s
         for (int st = 0; st < STEPS; ++st) qf[st] = u32x4{0, 0, 0, 0};
     }
 
-    // this lane's byte offsets into a K tile for the four contraction steps of a 128-byte group (key row n of a 32-key block,
+    // this lane's byte offsets into a K tile for the contraction steps of a 128- or 256-byte group (key row n of a 32-key block,
     // granule 2 q + hb), and into a V tile for the transposing reads of column block mb (key row 4 hb + (p >> 2) of a run of 16
     // keys, 8-byte chunk p & 3 of the 16 columns 32 mb + 16 mh .., p = lane % 16, mh = bit 4 of the lane)
-    int koff[4], voff[MB];
+    int koff[KQ], voff[MB];
 #pragma unroll
-    for (int q4 = 0; q4 < 4; ++q4) koff[q4] = n * KROW + KLoader::swizzled(n, 2 * q4 + hb) * 16;
+    for (int q = 0; q < KQ; ++q) koff[q] = n * KROW + KLoader::swizzled(n, 2 * q + hb) * 16;
     {
         const int p = lane & 15, mh = (lane >> 4) & 1, r = 4 * hb + (p >> 2);
 #pragma unroll
@@ -549,7 +550,7 @@ __device__ __forceinline__ void prefix_rows(const PrefixArgs& a, int wg, char* s
                 return u32x4{v0[0], v0[1], v1[0], v1[1]};
             }
             const int st = (i - N_V) >> 1, kb = (i - N_V) & 1;
-            return lds_read16(kt + kb * 32 * KROW + koff[st & 3] + (st >> 2) * 128);
+            return lds_read16(kt + kb * 32 * KROW + koff[st % KQ] + st / KQ * (KQ * 32));
         };
         __builtin_amdgcn_s_setprio(1);      // above the other half's vector phase, or the first LDS reads would wait for it
         u32x4 fb[LEAD];
