@@ -44,7 +44,10 @@ struct PrefixLayout {
     size_t off_stats, off_acc, total;
 };
 
-// Path and row groups of a part.
+// Path and row groups of a part.  Up to 16 rows the keys path, with more the rows path (fp32: 32 rows of the keys path).  16
+// sequences of 8192 own rows, 4 KV heads of 128 + 128, keys against rows path: 8 rows 37.9 and 40.1 us, 16 rows 39.2 and
+// 40.9 us, 24 and 32 rows (two groups, every key read twice) 61.6 and 41.1 us.  fp32, 4 rows behind 4097: 14.7 us with 16
+// rows in a workgroup, 17.0 us with 32; with 32 rows 20.2 us.
 int plan_rows(PartPlan* pt, bool bf16, int H_kv) {
     pt->by_length = pt->caches > 1 && pt->caches <= kPrefixMaxDealt;
     pt->path = pt->rows <= 16 ? 1 : (bf16 ? 0 : 2);
