@@ -12,9 +12,9 @@
 // a bound that no kept entry can lie below (from histograms of the chunks' maxima), and only the histogram bin in which the
 // threshold falls is ordered.  Rows whose filters keep more than the list holds take the general way, radix selections over the row.
 //
-// Measured (kernels alone, MI355X; blocks + pick): 512 rows of 100003 fp32 logits without filters 53.5 + 8.8 us, 3.8 TB/s where
+// Measured (kernels alone, MI355X; blocks + pick): 512 rows of 100003 fp32 logits without filters 49 + 8.8 us, 4.2 TB/s where
 // 5.1 is a copy's: thirteen 64-bit instructions per logit take half as long as the bytes; 128 rows of 131071 bf16 logits with
-// mixed settings 13.3 + 20 us, the second for the rows that keep about a thousand (3.5 us the bound, 2.2 the chunks, 3.5 their
+// mixed settings 13 + 20 us, the second for the rows that keep about a thousand (3.5 us the bound, 2.2 the chunks, 3.5 their
 // logits, 7 the thresholds: some fifteen barriers and LDS round trips); 8 rows of 32000 5 + 10 us, all of it latency.
 #pragma once
 #include "device_common.hpp"
@@ -250,11 +250,10 @@ __device__ __forceinline__ Found<V> find_prefix(const V* part, int n, int lane, 
     return f;
 }
 
-// One wavefront per block of 2048 logits, four blocks per workgroup.  The 32 logits of a lane are worked on side by side, which
-// takes 142 registers and leaves three wavefronts to a SIMD; held to 128 for four, with 20 spilled, 512 rows of 100003 take 64 us
-// instead of 67, held to 96 for five 66.
+// One wavefront per block of 2048 logits, four blocks per workgroup.  Seven wavefronts to a SIMD (72 registers) hide the reads behind the
+// exponentials: 512 rows of 100003 fp32 logits take 49 us; 53.5 with three (142 registers), 35.5 without the exponentials, 40 a copy's time.
 template <bool BF16>
-__global__ void __launch_bounds__(kThreads, 4) k_sample_blocks(const SampleArgs a) {
+__global__ void __launch_bounds__(kThreads, 7) k_sample_blocks(const SampleArgs a) {
     touch_args<SampleArgs>();
     const int lane = threadIdx.x & 63;
     const int row = a.div_wg.div((int)blockIdx.x);
@@ -301,7 +300,7 @@ __global__ void __launch_bounds__(kThreads, 4) k_sample_blocks(const SampleArgs 
 #pragma unroll
             for (int j = 0; j < 8; ++j)
 #pragma unroll
-                for (int k = 0; k < 4; ++k) part[k] += x[k][j] == M ? 1.0 : exp2_64(((double)x[k][j] - Md) * rule.c);
+                for (int k = 0; k < 4; ++k) part[k] += exp2_64(x[k][j] == M ? 0.0 : ((double)x[k][j] - Md) * rule.c);
         }
         sum = wave_sum((part[0] + part[1]) + (part[2] + part[3]));
     }
