@@ -22,7 +22,7 @@
 
 namespace ssv {
 
-struct SampleBlock { double sum, max; };     // of 2048 logits: sum of 2^(x c - e), c = log2(e) / t, e the whole number next to max c; maximum
+struct SampleBlock { double sum, max; };     // of 2048 logits: sum of 2^((x - max) c), c = log2(e) / t; maximum
 
 struct SampleArgs {
     const char* logits;
@@ -76,11 +76,12 @@ __device__ __forceinline__ double exp2_64(double y) {
     return __builtin_ldexp(p, (int)n);
 }
 
-// 2^(x c - e) for a whole number e, x c - e in [-1000, 1000], for sums over blocks: degree 8 (off by 1.1e-12 at most: such a shift of the
+// 2^(d c) for d c in [-1000, 0], 1 for d = 0, for sums over blocks: degree 8 (off by 1.1e-12 at most: such a shift of the
 // running sum moves a token in one of a million samples of the largest vocabulary), and without slow conversions: adding
-// 1.5 * 2^52 - e rounds to a whole number and leaves it in the low bits, from where it goes into the exponent.
-__device__ __forceinline__ double exp2_64_from(double x, double c, double magic_e) {
-    const double t = __builtin_fma(x, c, magic_e), f = __builtin_fma(x, c, magic_e - t);
+// 1.5 * 2^52 rounds to a whole number and leaves it in the low bits, from where it goes into the exponent.
+__device__ __forceinline__ double exp2_64_short(double d, double c) {
+    constexpr double MAGIC = 6755399441055744.0;
+    const double t = __builtin_fma(d, c, MAGIC), f = __builtin_fma(d, c, MAGIC - t);
     double p = 1.3255224878668817e-06;
     p = __builtin_fma(p, f, 1.5310079402249296e-05);
     p = __builtin_fma(p, f, 0.00015403455852453838);
@@ -95,21 +96,11 @@ __device__ __forceinline__ double exp2_64_from(double x, double c, double magic_
     return __builtin_bit_cast(double, (uint64_t)((uint32_t)(bits >> 32) + (n << 20)) << 32 | (uint32_t)bits);
 }
 
-// Whether 2^(x c - e) is within reach for a block of maximum M: not for temperatures of 1e35 and more, nor those below 1e-8 of the
-// maximum (nor M = +-inf); such blocks sum 2^((x - M) c).
-__device__ __forceinline__ bool whole_exponents(double M, double c) { return M - 1000.0 / c > -3e38 && fabs(M) * c < 3e8; }
-
 // Weight of a logit against a maximum; 1 at the maximum, whatever that is.
 struct SampleWeight {
     double M, c;       // c = log2(e) / temperature
     float Mf;
     __device__ __forceinline__ double operator()(float x) const { return exp2_64(x == Mf ? 0.0 : ((double)x - M) * c); }
-    // of a block of sum 1
-    __device__ __forceinline__ double of_block(double max) const {
-        if (!whole_exponents(max, c)) return (*this)((float)max);
-        const double e = __builtin_rint(max * c);
-        return exp2_64(whole_exponents(M, c) ? e - M * c : (max - M) * c + (e - max * c));
-    }
 };
 
 // The settings of a sequence as the header reads them.
@@ -132,7 +123,7 @@ __device__ __forceinline__ SampleRule sample_rule(const SampleArgs& a, int b) {
     r.by_k = r.top_k > 0 && r.top_k < a.V;
     r.by_p = r.top_p < 1.f;
     r.by_m = r.min_p > 0.f;
-    r.c = 1.4426950408889634 / (double)r.t;
+    r.c = fmax(1.4426950408889634 / (double)r.t, 1e-300);      // (an infinite temperature leaves finite differences without weight, and -inf without a chance)
     return r;
 }
 
@@ -287,20 +278,13 @@ __global__ void __launch_bounds__(kThreads, 7) k_sample_blocks(const SampleArgs 
             for (int k = 0; k < 4; ++k)
 #pragma unroll
                 for (int j = 0; j < 8; ++j) part[k] += x[k][j] == M ? 1.0 : 0.0;
-        } else if (whole_exponents(Md, rule.c)) {
-            // logits below M - 1000 / c weigh less than 2^-980 (the rounding of this bound to 24 bits moves the exponent by less than 20):
-            // they count as that, and a sum of 1/2 or more does not notice
-            const float low = (float)(Md - 1000.0 / rule.c);
-            const double magic_e = 6755399441055744.0 - __builtin_rint(Md * rule.c);
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-#pragma unroll
-                for (int k = 0; k < 4; ++k) part[k] += exp2_64_from((double)fmaxf(x[k][j], low), rule.c, magic_e);
         } else {
+            // logits below M - 1000 / c, and NaN, count as that: they weigh 2^-1000, and a sum of 1 or more does not notice
+            const double low = -1000.0 / rule.c;
 #pragma unroll
             for (int j = 0; j < 8; ++j)
 #pragma unroll
-                for (int k = 0; k < 4; ++k) part[k] += exp2_64(x[k][j] == M ? 0.0 : ((double)x[k][j] - Md) * rule.c);
+                for (int k = 0; k < 4; ++k) part[k] += exp2_64_short(fmax((double)x[k][j] - Md, low), rule.c);
         }
         sum = wave_sum((part[0] + part[1]) + (part[2] + part[3]));
     }
@@ -455,7 +439,7 @@ __global__ void __launch_bounds__(kSampleThreads) k_sample_pick(const SampleArgs
     if (rule.sums()) {
         for (int k = lane; k < a.n_blocks; k += 64) {
             const SampleBlock x = blocks[k];
-            const double v = x.sum == 0.0 ? 0.0 : x.sum * weight.of_block(x.max);
+            const double v = x.sum == 0.0 ? 0.0 : x.sum * weight((float)x.max);
             s_sum[k] = v;              // (every wavefront writes what it reads below: the same values)
             total += v;
         }

@@ -226,3 +226,34 @@ def test_largest_vocabulary_and_many_rows():
     x = logits(54, (700, 3, 257), "bf16")
     n = 700
     check(x, [0.9] * n, [0 if i % 3 else 7 for i in range(n)], [0.9 if i % 2 else 1.0 for i in range(n)], [0.0] * n, rng.random((n, 3)))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n", [2, 16, 200, 3000, 12000])
+def test_top_p_that_ends_on_a_border(n, dtype):
+    """n equal logits, all others out of reach: half of the mass is n / 2 entries, neither more nor fewer, whatever the logit and the
+    temperature (sums of equal weights are exact)."""
+    import torch
+    V = 3 * n + 5
+    x = torch.full((8, 1, V), -2000.0)
+    at = torch.randperm(V, generator=torch.Generator().manual_seed(n))[:n]
+    tops = [1000.0, 0.1, -3.7, 7.3e4, 1e-3, 12.34, 1000.0, -1e-30]
+    for b, top in enumerate(tops):
+        x[b, 0, at] = top
+    x = x.to(torch.bfloat16 if dtype == "bf16" else torch.float32).cuda()
+    t, p = [10.0, 0.7, 1.0, 3.0, 0.1, 1.3, 0.01, 1.0], [0.5, 0.25, 0.5, 0.75, 0.5, 0.5, 0.5, 0.25]
+    p = p if n % 4 == 0 else [0.5] * 8
+    for u in (0.3, 0.9999999):
+        check(x, t, [0] * 8, p, [0.0] * 8, [[u]] * 8)
+        check(x, t, [V - 1] * 8, p, [0.0] * 8, [[u]] * 8)
+
+
+def test_extreme_temperatures():
+    import torch
+    x = logits(61, (10, 2, 9000), "f32")
+    x[:, :, ::7] = float("-inf")
+    x[:, :, 3] = float("nan")
+    t = [float("inf"), 3e38, 1e30, 1e6, 1e-6, 1e-30, 1e-38, 1e-45, float("inf"), 1e-20]
+    for k, p, m in ((0, 1.0, 0.0), (50, 1.0, 0.0), (0, 0.3, 0.0), (0, 1.0, 0.5), (3000, 0.9, 0.0)):
+        check(x, t, [k] * 10, [p] * 10, [m] * 10, np.random.default_rng(61).random((10, 2)))
+    check(torch.sign(x) * 3e38, t, [0] * 10, [1.0] * 10, [0.0] * 10, np.random.default_rng(62).random((10, 2)))
