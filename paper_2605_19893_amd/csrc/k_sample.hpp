@@ -17,6 +17,8 @@
 // mixed settings 13 + 20 us, the second for the rows that keep about a thousand (3.5 us the bound, 2.2 the chunks, 3.5 their
 // logits, 7 the thresholds: some fifteen barriers and LDS round trips); 8 rows of 32000 5 + 10 us, all of it latency.
 #pragma once
+#include <type_traits>
+
 #include "device_common.hpp"
 #include "wave_ops.hpp"
 
@@ -484,19 +486,26 @@ __global__ void __launch_bounds__(kSampleThreads) k_sample_pick(const SampleArgs
     const uint16_t* maxima = a.maxima + (int64_t)row * a.n_blocks * kSampleChunks;
     const int n_groups8 = a.n_blocks * (kSampleChunks / 8);
     const int n_it = (n_groups8 + kSampleThreads - 1) / kSampleThreads;
-    // A thread has n_it consecutive groups of eight chunks, in order; eight groups at a time: body(first chunk, four pairs of halves each).
+    // A thread has n_it consecutive groups of eight chunks, in order; N groups at a time: body(first chunk, four pairs of halves each).  N
+    // is 8, so that the groups of a vocabulary of up to 262144 are fetched at once, or 2 where a thread has no more (up to 65536: a
+    // chain of eight over 32000 takes 13.8 us, 14.5 with the code of eight; mixed settings over 131071 33.4 us, 35.0 with that of two).
     auto fetch_max = [&](int it) { return *reinterpret_cast<const u32x4*>(maxima + 8 * min(tid * n_it + it, n_groups8 - 1)); };
     auto each_max = [&](auto&& body) {
+        auto run = [&](auto groups) {
+            constexpr int N = decltype(groups)::value;
 #pragma unroll 1
-        for (int it0 = 0; it0 < n_it; it0 += 8) {
-            u32x4 x[8];
+            for (int it0 = 0; it0 < n_it; it0 += N) {
+                u32x4 x[N];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) x[k] = it0 + k < n_it ? fetch_max(it0 + k) : u32x4{0, 0, 0, 0};
+                for (int k = 0; k < N; ++k) x[k] = it0 + k < n_it ? fetch_max(it0 + k) : u32x4{0, 0, 0, 0};
 #pragma unroll
-            for (int k = 0; k < 8; ++k)
-                if (it0 + k >= n_it || tid * n_it + it0 + k >= n_groups8) x[k] = u32x4{0, 0, 0, 0};
-            body(8 * (tid * n_it + it0), x);
-        }
+                for (int k = 0; k < N; ++k)
+                    if (it0 + k >= n_it || tid * n_it + it0 + k >= n_groups8) x[k] = u32x4{0, 0, 0, 0};
+                body(8 * (tid * n_it + it0), x);
+            }
+        };
+        if (n_it <= 2) run(std::integral_constant<int, 2>{});
+        else run(std::integral_constant<int, 8>{});
     };
     auto each_half = [&](auto&& body) {      // one by one (where the code's length counts more)
 #pragma unroll 1
@@ -577,9 +586,9 @@ __global__ void __launch_bounds__(kSampleThreads) k_sample_pick(const SampleArgs
         // the k-th largest of the maxima of groups of chunks, four per thread (the lower edge of its bin): as many logits are as large.  With
         // fewer groups the least of the maxima of all chunks, if there are k.
         u16x2 v2[4] = {};
-        each_max([&](int, const u32x4 (&x)[8]) {
+        each_max([&](int, const auto& x) {
 #pragma unroll
-            for (int k = 0; k < 8; ++k)
+            for (int k = 0; k < (int)(sizeof(x) / 16); ++k)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) v2[j] = __builtin_elementwise_max(v2[j], halves(x[k][j]));
         });
@@ -632,10 +641,10 @@ __global__ void __launch_bounds__(kSampleThreads) k_sample_pick(const SampleArgs
     // how many chunks' halves reach `half`; the chunks to `list` if they fit
     auto list_chunks = [&](uint32_t half, uint32_t* list) {
         const uint32_t less = half - 1;          // (half is 0x80 or more: that of the lowest finite key)
-        auto hits_of = [&](const u32x4 (&x)[8]) {
+        auto hits_of = [&](const auto& x) {
             uint64_t hits = 0;                   // bit 8 k + j: chunk j of group k
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
+            for (int k = 0; k < (int)(sizeof(x) / 16); ++k) {
                 uint32_t two = 0;                // bits 0, 2, 4, 6: the lower halves, 16, 18, ..: the upper ones
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
@@ -648,7 +657,7 @@ __global__ void __launch_bounds__(kSampleThreads) k_sample_pick(const SampleArgs
         };
         int mine = 0, n_hit;
         uint64_t hits;
-        each_max([&](int, const u32x4 (&x)[8]) { mine += __builtin_popcountll(hits = hits_of(x)); });
+        each_max([&](int, const auto& x) { mine += __builtin_popcountll(hits = hits_of(x)); });
         int to = block.scan(mine, n_hit);
         clear_bins();
         if (n_hit <= kSampleList) {
@@ -658,7 +667,7 @@ __global__ void __launch_bounds__(kSampleThreads) k_sample_pick(const SampleArgs
             if (n_it <= 8) {
                 put(8 * tid * n_it);
             } else {
-                each_max([&](int c, const u32x4 (&x)[8]) {
+                each_max([&](int c, const auto& x) {
                     hits = hits_of(x);
                     put(c);
                 });
