@@ -282,7 +282,7 @@ __global__ void __launch_bounds__(kThreads, 7) k_sample_blocks(const SampleArgs 
                 for (int j = 0; j < 8; ++j) part[k] += x[k][j] == M ? 1.0 : 0.0;
         } else {
             // logits below M - 1000 / c, and NaN, count as that: they weigh 2^-1000, and a sum of 1 or more does not notice
-            const double low = -1000.0 / rule.c;
+            const double low = fmax(-693.1471805599453 * (double)rule.t, -1e303);
 #pragma unroll
             for (int j = 0; j < 8; ++j)
 #pragma unroll
@@ -629,7 +629,9 @@ __global__ void __launch_bounds__(kSampleThreads) k_sample_pick(const SampleArgs
     } else if (rule.by_p) {
         // entries of weight below (1 - p) Z / V hold less than (1 - p) Z together
         const double least = (1.0 - (double)rule.top_p) * (1.0 - 1e-9) * total / (double)a.V;
-        const uint32_t k = order_key(mx == INFINITY ? mx : (float)((double)mx + log(least) * (double)rule.t));
+        // (a logarithm of 24 bits with 1e-5 to spare: least lies between 2^-45 and 1)
+        const float log2_least = __builtin_amdgcn_logf((float)least) * 1.00001f - 1e-5f;
+        const uint32_t k = order_key(mx == INFINITY ? mx : (float)((double)mx + (double)log2_least * 0.6931471805599453 * (double)rule.t));
         lo = max(lo, k > 2 ? k - 2 : 0);
     }
     if (rule.by_m && !rule.by_p) lo = max(lo, tau_m);
