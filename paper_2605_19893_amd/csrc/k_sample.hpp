@@ -12,10 +12,10 @@
 // a bound that no kept entry can lie below (from histograms of the chunks' maxima), and only the histogram bin in which the
 // threshold falls is ordered.  Rows whose filters keep more than the list holds take the general way, radix selections over the row.
 //
-// Measured (kernels alone, MI355X; blocks + pick): 512 rows of 100003 fp32 logits without filters 49 + 8.8 us, 4.2 TB/s where
+// Measured (kernels alone, MI355X; blocks + pick): 512 rows of 100003 fp32 logits without filters 47.5 + 8.5 us, 4.3 TB/s where
 // 5.1 is a copy's: thirteen 64-bit instructions per logit take half as long as the bytes; 128 rows of 131071 bf16 logits with
 // mixed settings 13 + 20 us, the second for the rows that keep about a thousand (3.5 us the bound, 2.2 the chunks, 3.5 their
-// logits, 7 the thresholds: some fifteen barriers and LDS round trips); 8 rows of 32000 5 + 10 us, all of it latency.
+// logits, 7 the thresholds: some fifteen barriers, LDS round trips and code that runs once); 8 rows of 32000 4.5 + 8 us, all of it latency.
 #pragma once
 #include <type_traits>
 
@@ -244,7 +244,7 @@ __device__ __forceinline__ Found<V> find_prefix(const V* part, int n, int lane, 
 }
 
 // One wavefront per block of 2048 logits, four blocks per workgroup.  Seven wavefronts to a SIMD (72 registers) hide the reads behind the
-// exponentials: 512 rows of 100003 fp32 logits take 49 us; 53.5 with three (142 registers), 35.5 without the exponentials, 40 a copy's time.
+// exponentials: 512 rows of 100003 fp32 logits take 47.5 us; 53.5 with three (142 registers), 35.5 without the exponentials, 40 a copy's time.
 template <bool BF16>
 __global__ void __launch_bounds__(kThreads, 7) k_sample_blocks(const SampleArgs a) {
     touch_args<SampleArgs>();
