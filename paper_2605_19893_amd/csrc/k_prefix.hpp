@@ -724,10 +724,12 @@ struct PrefixCombineArgs {
 };
 
 // out = sum_s 2^(m_s - M) acc_s / sum_s 2^(m_s - M) Z_s over the slices that saw a key; DV / 4 threads per row.  The small calls
-// are bound by latency: a lane of the row's group fetches the statistics of its own slots while the first eight slots' sums are
-// on their way, the maximum and the total go through lane exchanges, and every later batch of eight is fetched at once.
+// are bound by latency: a lane of the row's group fetches the statistics of its own slots while (EARLY) the first eight slots' sums
+// are on their way, the maximum and the total go through lane exchanges, and every later batch of eight is fetched at once.
 // Measured: 3.9 us for 256 rows, 5.5 us for 2048 (22 MB of partial states), 21.5 us for 32768 (121 MB, 5.6 TB/s).
-template <bool BF16, int DV>
+// EARLY: the first eight slots' sums are fetched before it is known which of them count; else (many rows, which hide the second
+// round trip) only those that do.
+template <bool BF16, int DV, bool EARLY>
 __global__ void __launch_bounds__(kThreads) k_prefix_combine(const PrefixCombineArgs a) {
     touch_args<PrefixCombineArgs>();
     constexpr int TPR = DV / 4, RPW = kThreads / TPR, PER = kPrefixMaxSlots / TPR, BATCH = 8;
@@ -746,7 +748,7 @@ __global__ void __launch_bounds__(kThreads) k_prefix_combine(const PrefixCombine
     const int64_t step = a.rows_total * DV;
     f32x4 v[BATCH];
 #pragma unroll
-    for (int s = 0; s < BATCH; ++s) v[s] = *reinterpret_cast<const f32x4*>(at + min(s, a.n_slots - 1) * step);
+    for (int s = 0; s < BATCH; ++s) v[s] = EARLY ? *reinterpret_cast<const f32x4*>(at + min(s, a.n_slots - 1) * step) : f32x4{0.f, 0.f, 0.f, 0.f};
     float M = -INFINITY, Z = 0.f;
 #pragma unroll
     for (int k = 0; k < PER; ++k)
@@ -765,12 +767,12 @@ __global__ void __launch_bounds__(kThreads) k_prefix_combine(const PrefixCombine
 #pragma unroll
     for (int k = 0; k < PER; ++k)
         for (int s0 = k * TPR; s0 < (k + 1) * TPR && s0 < a.n_slots; s0 += BATCH) {
-            // slots that saw no key, or that do not exist, hold anything: their weight is 0, and from the second batch on they are not fetched
+            // slots that saw no key, or that do not exist, hold anything: their weight is 0, and but for an early first batch they are not fetched
             float ws[BATCH];
 #pragma unroll
             for (int s = 0; s < BATCH; ++s) {
                 ws[s] = __shfl(w[k], s0 - k * TPR + s, TPR);
-                if (s0 && ws[s] != 0.f) v[s] = *reinterpret_cast<const f32x4*>(at + (s0 + s) * step);
+                if ((s0 || !EARLY) && ws[s] != 0.f) v[s] = *reinterpret_cast<const f32x4*>(at + (s0 + s) * step);
             }
 #pragma unroll
             for (int s = 0; s < BATCH; ++s)

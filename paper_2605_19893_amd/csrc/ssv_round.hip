@@ -273,7 +273,11 @@ int prefix_launch(const void* q, const void* kp, const void* vp, const void* k, 
     c.div_H = FastDiv::of(p->H);
     c.div_T = FastDiv::of(p->T);
     for (int j = 0; j < 3; ++j) c.out_s[j] = lo.out_s[j];
-    hipLaunchKernelGGL((k_prefix_combine<BF16, DV>), dim3(ceil_div(lo.rows_total, kThreads / (DV / 4))), dim3(kThreads), 0, stream, c);
+    // Up to two workgroups per CU fetch sums before they know whether they count, more of them only what counts: 4096 rows of 128 5.5
+    // and 6.3 us, 8192 rows 9.8 and 9.6, 12800 rows (four slots of eight in use) 10.3 and 6.2, 22848 rows 16 and 9.4.
+    const int wgs = ceil_div(lo.rows_total, kThreads / (DV / 4));
+    if (wgs <= 2 * kPrefixWgs) hipLaunchKernelGGL((k_prefix_combine<BF16, DV, true>), dim3(wgs), dim3(kThreads), 0, stream, c);
+    else hipLaunchKernelGGL((k_prefix_combine<BF16, DV, false>), dim3(wgs), dim3(kThreads), 0, stream, c);
     return hipGetLastError() == hipSuccess ? SSV_OK : SSV_ELAUNCH;
 }
 

@@ -292,3 +292,11 @@ def test_bounds_far_above_the_lengths(shape, B, T):
     args, h = setup(41, shape, B=B, T=T, H=4, Hk=1, G=1, plens=[129], lens=[(7 * b) % 90 for b in range(B)], P=60000, S=4000)
     call(args)
     check(args, h)
+
+
+@pytest.mark.parametrize("shape, T", [("bf16_128", 70), ("bf16_64", 110), ("f32_64", 110)])
+def test_more_rows_than_two_joining_workgroups_per_unit(shape, T):
+    """Rows enough that their sums are fetched only where they count; sequences without nodes, slices without keys."""
+    args, h = setup(42, shape, B=6, T=T, H=16, Hk=1, G=2, plens=[40, 200], lens=[0, 70, 1, 33, 5, 0], nq=[T, T, 0, T, T - 1, T], P=200, S=600)
+    call(args)
+    check(args, h)
