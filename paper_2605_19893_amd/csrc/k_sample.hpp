@@ -125,7 +125,7 @@ __device__ __forceinline__ SampleRule sample_rule(const SampleArgs& a, int b) {
     r.by_k = r.top_k > 0 && r.top_k < a.V;
     r.by_p = r.top_p < 1.f;
     r.by_m = r.min_p > 0.f;
-    r.c = fmax(1.4426950408889634 / (double)r.t, 1e-300);      // (an infinite temperature leaves finite differences without weight, and -inf without a chance)
+    r.c = fmax(1.4426950408889634 / (double)r.t, 1e-300);      // (infinite temperature: every finite logit weighs the same, -inf nothing)
     return r;
 }
 
