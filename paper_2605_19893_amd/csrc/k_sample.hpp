@@ -38,7 +38,6 @@ struct SampleArgs {
     int wg_per_row;        // k_sample_blocks
     FastDiv div_wg, div_T;
     int64_t s[2];          // bytes: sequence, node
-    double mass_scale;     // fixed-point units of a weight of 1: V times it stays below 2^63
 };
 
 constexpr int kSampleThreads = 512, kSampleWaves = kSampleThreads / 64;     // of k_sample_pick
@@ -518,9 +517,13 @@ __global__ void __launch_bounds__(kSampleThreads) k_sample_pick(const SampleArgs
             }
         }
     };
-    // A weight in fixed point, 2^-42 of the largest or finer (2^62 shared by the vocabulary): sums of these do not depend on the order
-    // of the atomics.
-    auto mass = [&](uint32_t k) { return (uint64_t)(weight(key_value(k)) * a.mass_scale + 0.5); };
+    // A weight in fixed point: sums of these do not depend on the order of the atomics.  The unit is the power of two that brings the sum of
+    // what is added up to 2^62 .. 2^63, so that V roundings to it are at most V 2^-63 of that sum, however peaked the row is.  (A unit
+    // made for V weights of 1 leaves the tail of a peaked row a few bits: of 2^20 entries behind a peak, of which top-p 0.9999999 keeps
+    // 214736, it kept 11000 fewer.)  Without top-k the sum is the row's, known from its blocks.
+    auto mass_scale_of = [](double sum) { return __builtin_ldexp(1.0, 63 - __builtin_amdgcn_frexp_exp(sum)); };      // sum below 2^exp
+    double mass_scale = rule.by_p && !rule.by_k ? mass_scale_of(total) : 0.0;
+    auto mass = [&](uint32_t k) { return (uint64_t)(weight(key_value(k)) * mass_scale + 0.5); };
     auto clear_bins = [&] {              // (a barrier follows before they are used)
         if (tid < kSampleBins) {
             s_mass[tid] = 0;
@@ -705,7 +708,7 @@ __global__ void __launch_bounds__(kSampleThreads) k_sample_pick(const SampleArgs
             each_half(count);
         }
         __syncthreads();
-        half = max(half, bin_edge(find_bin(by_mass, (uint32_t)rule.top_k, (double)rule.top_p * (1.0 + 1e-9) * total * a.mass_scale), shift));
+        half = max(half, bin_edge(find_bin(by_mass, (uint32_t)rule.top_k, (double)rule.top_p * (1.0 + 1e-9) * total * mass_scale), shift));
         lo = max(lo, half << 16);
         if (fits) {
             int mine = 0;
@@ -786,6 +789,7 @@ __global__ void __launch_bounds__(kSampleThreads) k_sample_pick(const SampleArgs
     auto entry = [&](int k) { return s_list[l0 + k]; };
     uint64_t last_kept = 0;             // the last entry that is kept
     if (listed && (rule.by_k || rule.by_p)) {
+        if (rule.by_k) mass_scale = 2.0 * mass_scale_of((double)n);      // (n weights of at most 1, sums below 2^64; off by n^2 2^-64 of the kept sum, 1 or more, at most)
         // ---- the exact threshold: a histogram of the list, and the entries of the bin in which it falls in order
         each_of(l1 - l0, q, entry, [&](int, uint64_t x) {
             const int at = bin_of(entry_value(x));
@@ -853,7 +857,7 @@ __global__ void __launch_bounds__(kSampleThreads) k_sample_pick(const SampleArgs
             return n_below;
         };
         // by count, then by mass if that ends in another bin, or by mass alone
-        double target = (double)rule.top_p * total * a.mass_scale;
+        double target = (double)rule.top_p * total * mass_scale;
         bool of_mass = !rule.by_k;
 #pragma unroll 1
         for (;;) {
@@ -901,7 +905,7 @@ __global__ void __launch_bounds__(kSampleThreads) k_sample_pick(const SampleArgs
     }
 
     // ---- the general way: radix selections over the row, re-read for every digit.  tau of top-k is selected by counts, tau of top-p by
-    //      mass; masses are summed as 64-bit fixed point, so the sums do not depend on the order of the atomics.
+    //      mass.
     __syncthreads();
     double* s_sums = reinterpret_cast<double*>(s_mem);
     uint32_t* s_cnt = reinterpret_cast<uint32_t*>(s_mem + kSampleMaxIters * kSampleWaves * 8);
@@ -972,6 +976,16 @@ __global__ void __launch_bounds__(kSampleThreads) k_sample_pick(const SampleArgs
     }
     if (rule.by_p) {
         const uint32_t tau_k = tau, quota_k = quota;
+        if (rule.by_k) {                 // the sum over the first top_k entries, for the unit
+            double sum = 0.0, all;
+            each([&](int, int, const float (&x)[8]) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (order_key(x[j]) > tau_k) sum += weight(x[j]);
+            });
+            block.scan(sum, all);
+            mass_scale = mass_scale_of(all + (double)quota_k * weight(key_value(tau_k)));
+        }
         unsigned long long above = 0;
         uint32_t prefix = 0;
         double target = 0.0;

@@ -364,9 +364,6 @@ int ssv_sample(const void* logits, const float* temperature, const int32_t* top_
     a.wg_per_row = ceil_div(a.n_blocks, kThreads / 64);
     a.div_wg = FastDiv::of(a.wg_per_row);
     a.div_T = FastDiv::of(p->T);
-    int bits = 0;
-    while ((1 << bits) < p->V) ++bits;
-    a.mass_scale = std::ldexp(1.0, 62 - bits);
     const dim3 grid(p->B * p->T * a.wg_per_row), rows(p->B * p->T);
     if (p->dtype == SSV_BF16) {
         hipLaunchKernelGGL(k_sample_blocks<true>, grid, dim3(kThreads), 0, (hipStream_t)stream, a);

@@ -257,3 +257,40 @@ def test_extreme_temperatures():
     for k, p, m in ((0, 1.0, 0.0), (50, 1.0, 0.0), (0, 0.3, 0.0), (0, 1.0, 0.5), (3000, 0.9, 0.0)):
         check(x, t, [k] * 10, [p] * 10, [m] * 10, np.random.default_rng(61).random((10, 2)))
     check(torch.sign(x) * 3e38, t, [0] * 10, [1.0] * 10, [0.0] * 10, np.random.default_rng(62).random((10, 2)))
+
+
+def kept_by_mass(x, top_k, top_p):
+    """(entries that top_k and top_p keep of a row at temperature 1, distance of the target from the nearest border in entries), in
+    numbers of 64 bits of mantissa: 2^20 roundings of a running sum of 53 are as large as a weight of e^-30."""
+    big = np.longdouble
+    ws = np.sort(np.exp(x.astype(big) - big(x.max())))[::-1]
+    if 0 < top_k < len(ws):
+        ws = ws[:top_k]
+    upto = np.cumsum(ws)
+    target = big(np.float32(top_p)) * upto[-1]
+    n = int(np.sum(upto < target)) + 1
+    return n, float(min(upto[n - 1] - target, target - (upto[n - 2] if n > 1 else 0)) / ws[n - 1])
+
+
+@pytest.mark.parametrize("V, top_k", [(1 << 20, 0), (1 << 20, (1 << 20) - 1), (1 << 20, 700000), (60000, 0), (1 << 20, 4000), (1 << 20, 500)])
+def test_top_p_near_one_behind_a_peak(V, top_k):
+    """One likely token and a long tail of weights about 2^-43 (where top_k cuts the tail short: 2^-34 and more), in descending order:
+    the last kept entry, which u = 1 asks for, says how many were kept.  The filters' sums are off by V 2^-63 of the whole at most, with a short
+    list of top_k by 2^-40 (half a unit for every one of its entries, were they all rounded the same way), the target and the row's sum by 2^-50."""
+    import torch
+    few = 0 < top_k < 10000
+    x = torch.full((V,), -100.0)
+    x[0] = 0.0
+    if few:        # as many alike as are kept at most
+        x[1:top_k + 1] = -23.6 if top_k > 1000 else -21.5
+    else:
+        shift = np.log(2.0 ** 20 / V)
+        x[1:] = torch.linspace(-29.0 + shift, -30.0 + shift, V - 1)
+    x = x.reshape(1, 1, V)
+    for top_p in (0.9999999, 1.0 - 2.0 ** -24):
+        n, off = kept_by_mass(x[0, 0].numpy(), top_k, top_p)
+        w = float(np.exp(x[0, 0, n - 1].double().item()))
+        slack = ((2.0 ** -40 if few else V * 2.0 ** -63) + 2.0 ** -50) / w
+        tok, pr = run(x.cuda(), [1.0], [top_k], [top_p], [0.0], [[1.0]])
+        assert 1 < n < (top_k or V)
+        assert abs(tok[0, 0] + 1 - n) <= (np.ceil(slack) if off < slack else 0)
