@@ -570,10 +570,23 @@ __global__ void __launch_bounds__(kSampleThreads) k_sample_pick(const SampleArgs
         if (rule.min_p >= 1.f) {
             tau_m = order_key(mx);
         } else {
-            // the lowest key of weight min_p or more: within a few units of the key of M + t ln(min_p)
+            // The lowest key of weight min_p or more, 64 keys looked at at once.  It lies within a few units of the key of M + t ln(min_p), but
+            // where M and t ln(min_p) cancel: what is left may be off by thousands of units, and the border is looked for between
+            // -inf, which weighs nothing, and the maximum, in six steps at most.
             const uint32_t k0 = order_key((float)((double)mx + log((double)rule.min_p) * (double)rule.t));
-            const uint64_t reach = __builtin_amdgcn_ballot_w64(weight(key_value(k0 + (uint32_t)lane - 32u)) >= (double)rule.min_p);
-            tau_m = reach ? k0 + (uint32_t)__builtin_ctzll(reach) - 32u : order_key(mx);
+            uint64_t reach = __builtin_amdgcn_ballot_w64(weight(key_value(k0 + (uint32_t)lane - 32u)) >= (double)rule.min_p);
+            tau_m = k0 + (uint32_t)__builtin_ctzll(reach | 1ull << 63) - 32u;
+            if (!reach || (reach & 1u)) {                      // (uniform)
+                uint32_t below = order_key(-INFINITY);
+                tau_m = order_key(mx);
+                while (tau_m - below > 1u) {                   // (each step leaves a 64th of what lies between)
+                    const uint32_t step = (tau_m - below + 63u) / 64u, k = min(below + step * (uint32_t)(lane + 1), tau_m);
+                    reach = __builtin_amdgcn_ballot_w64(k == tau_m || weight(key_value(k)) >= (double)rule.min_p);
+                    const uint32_t first = (uint32_t)__builtin_ctzll(reach);      // (the last lane's key is tau_m)
+                    tau_m = min(below + step * (first + 1u), tau_m);
+                    below += step * first;
+                }
+            }
         }
     }
     const uint32_t lowest = order_key(-3.4028235e38f);      // (entries of -inf are never kept)

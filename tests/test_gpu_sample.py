@@ -294,3 +294,22 @@ def test_top_p_near_one_behind_a_peak(V, top_k):
         tok, pr = run(x.cuda(), [1.0], [top_k], [top_p], [0.0], [[1.0]])
         assert 1 < n < (top_k or V)
         assert abs(tok[0, 0] + 1 - n) <= (np.ceil(slack) if off < slack else 0)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_min_p_whose_border_is_zero(dtype):
+    """Settings for which M + t ln(min_p) is zero but for a trillionth: its rounding in 64 bits is thousands of 32-bit steps there."""
+    import torch
+    rows = [(0.1, 1.2476844787597656, 0.5418624877929688), (0.1, 3.2534255981445312, 1.4129447937011719), (0.1, 41.04684829711914, 17.826419830322266),
+            (0.05, 2.2117958068847656, 0.7383155822753906), (0.05, 11.779285430908203, 3.9320220947265625), (0.02, 13.251354217529297, 3.387340545654297),
+            (0.7, 1.9285774230957031, 5.407100677490234), (0.7, 19.910770416259766, 55.82329177856445), (0.5, 31.799739837646484, 45.87732696533203),
+            (0.25, 8.473453521728516, 6.1123046875), (0.9, 3.0236740112304688, 28.698352813720703), (0.0625, 4.0, 1.4426950408889634)]
+    m, top, t = (list(c) for c in zip(*rows))
+    B = len(rows)
+    x = torch.linspace(-0.995, 0.975, 198).repeat(B, 4, 1) * torch.tensor(top)[:, None, None]      # (no value within a thousandth of the border)
+    x = torch.cat([x, torch.tensor(top)[:, None, None].expand(B, 4, 1)], 2)
+    x = x.bfloat16() if dtype == "bf16" else x
+    u = [[0.05, 0.35, 0.65, 0.95]] * B
+    check(x.cuda(), t, [0] * B, [1.0] * B, m, u)
+    check(x.cuda(), t, [150] * B, [1.0] * B, m, u)
+    check(x.cuda(), t, [0] * B, [0.9] * B, m, u)
