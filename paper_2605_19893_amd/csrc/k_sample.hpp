@@ -13,7 +13,7 @@
 // threshold falls is ordered.  Rows whose filters keep more than the list holds take the general way, radix selections over the row.
 //
 // Measured (kernels alone, MI355X; blocks + pick): 512 rows of 100003 fp32 logits without filters 47.5 + 8.5 us, 4.3 TB/s where
-// 5.1 is a copy's: thirteen 64-bit instructions per logit take half as long as the bytes; 128 rows of 131071 bf16 logits with
+// 5.1 is a copy's: fifteen 64-bit instructions per logit take half as long as the bytes; 128 rows of 131071 bf16 logits with
 // mixed settings 13 + 20 us, the second for the rows that keep about a thousand (3.5 us the bound, 2.2 the chunks, 3.5 their
 // logits, 7 the thresholds: some fifteen barriers, LDS round trips and code that runs once); 8 rows of 32000 4.5 + 8 us, all of it latency.
 #pragma once
@@ -58,11 +58,8 @@ __device__ __forceinline__ uint32_t order_key(float x) {
 }
 __device__ __forceinline__ float key_value(uint32_t k) { return __uint_as_float(k ^ ((k >> 31) ? 0x80000000u : 0xffffffffu)); }
 
-// 2^y for y <= 0 (lower than -1100, -inf and NaN count as -1100, which gives 0): 2^n times the polynomial of degree 10 that takes the values of
-// 2^f at the eleven Chebyshev points of [-1/2, 1/2], off by at most 4e-16.  Eighteen instructions at the rate of 32-bit ones.
-__device__ __forceinline__ double exp2_64(double y) {
-    y = fmax(y, -1100.0);
-    const double n = __builtin_rint(y), f = y - n;
+// 2^f, f in [-1/2, 1/2]: the polynomial of degree 10 that takes the values of 2^f at the eleven Chebyshev points, off by at most 4e-16.
+__device__ __forceinline__ double exp2_near_0(double f) {
     double p = 7.072585949269223e-09;
     p = __builtin_fma(p, f, 1.0208690299958306e-07);
     p = __builtin_fma(p, f, 1.321544258792169e-06);
@@ -73,26 +70,22 @@ __device__ __forceinline__ double exp2_64(double y) {
     p = __builtin_fma(p, f, 0.05550410866444772);
     p = __builtin_fma(p, f, 0.24022650695910097);
     p = __builtin_fma(p, f, 0.69314718055995);
-    p = __builtin_fma(p, f, 1.0);
-    return __builtin_ldexp(p, (int)n);
+    return __builtin_fma(p, f, 1.0);
 }
 
-// 2^(d c) for d c in [-1000, 0], 1 for d = 0, for sums over blocks: degree 8 (off by 1.1e-12 at most: such a shift of the
-// running sum moves a token in one of a million samples of the largest vocabulary), and without slow conversions: adding
-// 1.5 * 2^52 rounds to a whole number and leaves it in the low bits, from where it goes into the exponent.
+// 2^y for y <= 0 (lower than -1100, -inf and NaN count as -1100, which gives 0).  Eighteen instructions at the rate of 32-bit ones.
+__device__ __forceinline__ double exp2_64(double y) {
+    y = fmax(y, -1100.0);
+    const double n = __builtin_rint(y);
+    return __builtin_ldexp(exp2_near_0(y - n), (int)n);
+}
+
+// 2^(d c) for d c in [-1000, 0], 1 for d = 0, for sums over blocks, without slow conversions: adding 1.5 * 2^52 rounds to a whole
+// number and leaves it in the low bits, from where it goes into the exponent.
 __device__ __forceinline__ double exp2_64_short(double d, double c) {
     constexpr double MAGIC = 6755399441055744.0;
-    const double t = __builtin_fma(d, c, MAGIC), f = __builtin_fma(d, c, MAGIC - t);
-    double p = 1.3255224878668817e-06;
-    p = __builtin_fma(p, f, 1.5310079402249296e-05);
-    p = __builtin_fma(p, f, 0.00015403455852453838);
-    p = __builtin_fma(p, f, 0.0013333450568000645);
-    p = __builtin_fma(p, f, 0.009618129159402558);
-    p = __builtin_fma(p, f, 0.05550410941205933);
-    p = __builtin_fma(p, f, 0.2402265069581299);
-    p = __builtin_fma(p, f, 0.6931471805459335);
-    p = __builtin_fma(p, f, 1.0);
-    const uint64_t bits = __builtin_bit_cast(uint64_t, p);
+    const double t = __builtin_fma(d, c, MAGIC);
+    const uint64_t bits = __builtin_bit_cast(uint64_t, exp2_near_0(__builtin_fma(d, c, MAGIC - t)));
     const uint32_t n = (uint32_t)__builtin_bit_cast(uint64_t, t);
     return __builtin_bit_cast(double, (uint64_t)((uint32_t)(bits >> 32) + (n << 20)) << 32 | (uint32_t)bits);
 }

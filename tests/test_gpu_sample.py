@@ -313,3 +313,33 @@ def test_min_p_whose_border_is_zero(dtype):
     check(x.cuda(), t, [0] * B, [1.0] * B, m, u)
     check(x.cuda(), t, [150] * B, [1.0] * B, m, u)
     check(x.cuda(), t, [0] * B, [0.9] * B, m, u)
+
+
+def test_block_sums_are_good_to_64_bits():
+    """A border at u = 1/2 to within 2e-13 of the sum, between two blocks: 2048 logits whose exponentials are alike, and as much and a
+    little less (or more) beside the maximum itself.  The sums of a block take eleven additions and an exponential of
+    4e-16, the row's a few more: together below 2e-15 of the sum."""
+    import math
+    import torch
+    f32 = lambda v: float(np.float32(v))
+    V = 8192
+    for k, d in enumerate(f32(v) for v in -math.log(2) * np.array([0.02, 0.13, 0.25, 0.36, 0.47, 0.5, 0.62, 0.75, 0.88, 0.98, 1.3, 1.5])):
+        for eta in (8e-13, -8e-13):
+            # block 0: 0 and 2047 logits at d; blocks 1 and 2: as many of -0.05 as fit, then a few that make up the difference; block 3: nothing
+            first = 1.0 + 2047.0 * math.exp(d)
+            want = first * (1.0 - eta)
+            y = f32(-0.05)
+            count = int(want / math.exp(y))
+            values, left = [y] * count, want - count * math.exp(y)
+            while left > 1e-15 * want:
+                v = float(np.nextafter(np.float32(math.log(left)), np.float32(-np.inf)))
+                values.append(v)
+                left -= math.exp(v)
+            x = np.full(V, -np.inf, np.float32)
+            x[0], x[1:2048] = 0.0, d
+            x[2048:2048 + len(values)] = values
+            big = np.exp(x.astype(np.longdouble))
+            margin = float((big[:2048].sum() - big[2048:].sum()) / big.sum() / 2)
+            assert 1e-13 < abs(margin) < 2.0 ** -40 and (margin > 0) == (eta > 0)
+            tok, _ = run(torch.from_numpy(x).cuda().reshape(1, 1, V), [1.0], None, None, None, [[0.5]])
+            assert (tok[0, 0] < 2048) == (margin > 0), (k, d, eta, tok[0, 0], margin)
