@@ -49,7 +49,8 @@ typedef struct ssv_prefix_params {
  *   workspace: >= ssv_prefix_workspace_bytes(p) bytes, 256-byte aligned; contents need not be preserved or initialised;
  *   calls sharing a workspace must not overlap in time.
  * Scores, softmax statistics and sums are fp32; with bf16 inputs the probabilities are rounded to bf16 for the matrix
- * instructions, the result is rounded once to the type of out.
+ * instructions, the result is rounded once to the type of out.  Scores times the scale stay within +-2^27: a reference maximum
+ * is subtracted in fp32, and its rounding is a factor of all weights of a row, which has to stay in range.
  */
 int ssv_prefix_verify(const void* q, const void* k_prefix, const void* v_prefix, const void* k, const void* v,
                       const int32_t* prefix_lens, const int32_t* seq_lens, const int32_t* n_query, const int32_t* tree_parents,

@@ -392,7 +392,8 @@ __device__ __forceinline__ void prefix_keys(const PrefixArgs& a, int wg, char* s
 #pragma unroll
         for (int o = 0; o < kPrefixWaves; ++o)
             if (!(s_z[o][rb * 16 + n] == 0.f)) Z += s_z[o][rb * 16 + n] * fast_exp2(s_m[o][rb * 16 + n] - M);
-        const float f = z[rb] == 0.f ? 0.f : fast_exp2(mref[rb] * a.scale_log2 - M);
+        // (the maximum as it was rounded for Z: the product taken again would go into one instruction with the difference, unrounded)
+        const float f = z[rb] == 0.f ? 0.f : fast_exp2(s_m[wave][rb * 16 + n] - M);
         const int64_t slot = (int64_t)(pt.slot0 + w.slice) * a.rows_total;
         if (wave == 0 && G == 0 && valid[rb]) put_statistics(a, pt, w, prefix_state_row(a, row[rb]), M, Z);
         if (t0 >= t1) continue;                      // (uniform) an empty slice leaves Z = 0 and no sums

@@ -300,3 +300,24 @@ def test_more_rows_than_two_joining_workgroups_per_unit(shape, T):
     args, h = setup(42, shape, B=6, T=T, H=16, Hk=1, G=2, plens=[40, 200], lens=[0, 70, 1, 33, 5, 0], nq=[T, T, 0, T, T - 1, T], P=200, S=600)
     call(args)
     check(args, h)
+
+
+@pytest.mark.parametrize("T", [2, 9])
+@pytest.mark.parametrize("shape", sorted(SHAPES))
+def test_largest_scores_pick_the_largest(shape, T):
+    """Scores of 2^25.6 after scaling, whole numbers before it: products and sums are exact, the keys of the largest score share the weight
+    and all others vanish (the next is 2^15 lower).  The result is the mean of their values, rounded as probabilities and results are."""
+    import torch
+    scale = 2.0 ** 15
+    args, h = setup(45, shape, B=2, T=T, H=4, Hk=1, G=1, plens=[300], lens=[150, 20], garbage=False, scale=scale)
+    for at, name, top in ((0, "q", 9), (1, "kp", 8), (3, "k", 8)):
+        h[name] = np.random.default_rng(at).integers(-top, top + 1, h[name].shape).astype(np.float64)
+        h[name][..., 48:64], h[name][..., 64:] = top, 0.0
+        args[at].copy_(torch.from_numpy(h[name]))
+    call(args)
+    torch.cuda.synchronize()
+    got = args[10].double().cpu().numpy()
+    want, mass, _ = ro.prefix_attention(h["q"], h["kp"], h["vp"], h["k"], h["v"], h["plens"], h["lens"], h["nq"], h["parents"], scale)
+    assert scale * np.abs(h["kp"][0, 0] @ h["q"][0, 0, 0]).max() > 2.0 ** 25
+    rnd = 2.0 ** -8 if h["dt"] == "bf16" else 2.0 ** -24
+    assert (np.abs(got - want) <= rnd * (mass + np.abs(want)) + 2.0 ** -22 * mass).all()
