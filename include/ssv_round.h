@@ -28,7 +28,7 @@ typedef struct ssv_prefix_params {
     int32_t d_k, d_v;         /* head dims; supported (dtype, d_k, d_v): those of ssv_nsa_supported */
     int32_t n_prefix;         /* prefixes; B % n_prefix == 0: sequence b reads prefix b / (B / n_prefix) */
     int32_t dtype;            /* SSV_F32 or SSV_BF16: type of q, all K and V, out */
-    float   scale;            /* softmax scale, 2^-100 or more; 0 => 1/sqrt(d_k) */
+    float   scale;            /* softmax scale, 2^-100 to 2^100; 0 => 1/sqrt(d_k) */
     int32_t max_prefix_len;   /* host-side bound on prefix_lens[g]: rows of k_prefix / v_prefix per (prefix, KV head); 0: no prefix */
     int32_t max_seq_len;      /* host-side bound on seq_lens[b]; k and v hold at least max_seq_len + T rows per (sequence, KV head) */
     int64_t kp_stride[3], vp_stride[3];   /* elements: prefix, KV head, row */

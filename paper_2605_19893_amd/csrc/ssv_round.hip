@@ -146,7 +146,7 @@ int prefix_layout(const ssv_prefix_params* p, PrefixLayout* lo) {
     if (p->dtype != SSV_F32 && p->dtype != SSV_BF16) return SSV_EINVAL;
     if (p->max_prefix_len < 0 || p->max_seq_len < 0 || !(p->scale >= 0.f) || std::isinf(p->scale)) return SSV_EINVAL;
     const int H_g = p->H / p->H_kv;
-    if (p->T > SSV_MAX_T || (p->scale > 0.f && p->scale < 0x1p-100f)) return SSV_EUNSUPPORTED;      // (scale * log2(e) stays normal)
+    if (p->T > SSV_MAX_T || (p->scale > 0.f && !(p->scale >= 0x1p-100f && p->scale <= 0x1p100f))) return SSV_EUNSUPPORTED;      // (scale * log2(e) stays normal)
     if (H_g != 1 && H_g != 2 && H_g != 4 && H_g != 8 && H_g != 16) return SSV_EUNSUPPORTED;
     if (!ssv_nsa_supported(p->dtype, p->d_k, p->d_v)) return SSV_EUNSUPPORTED;
     if (p->max_seq_len > INT32_MAX - SSV_MAX_T - 64 || p->max_prefix_len > INT32_MAX - 64) return SSV_EUNSUPPORTED;

@@ -233,3 +233,11 @@ def test_prefix_refuses_scales_below_2_to_the_minus_100():
     assert B.ssv_prefix_workspace_bytes(prefix_params(scale=2.0 ** -100)) > 0
     test_prefix_refusals(dict(scale=2.0 ** -101), B.SSV_EUNSUPPORTED)
     test_prefix_refusals(dict(scale=1e-40), B.SSV_EUNSUPPORTED)
+
+
+def test_prefix_refuses_scales_above_2_to_the_100():
+    """A scale whose product with log2(e) is not finite made every row a NaN."""
+    assert B.ssv_prefix_workspace_bytes(prefix_params(scale=2.0 ** 100)) > 0
+    test_prefix_refusals(dict(scale=2.0 ** 100 * (1 + 2.0 ** -23)), B.SSV_EUNSUPPORTED)
+    test_prefix_refusals(dict(scale=2.5e38), B.SSV_EUNSUPPORTED)
+    test_prefix_refusals(dict(scale=3.4e38), B.SSV_EUNSUPPORTED)
