@@ -12,6 +12,7 @@
  * Draft nodes as in ssv_nsa.h: node i of sequence b occupies slot seq_lens[b] + i; tree_parents[b*T+i] is -1 (child of the
  * last committed token) or the index (< i) of its parent (other values count as -1); NULL: a chain.  n_query[b] (NULL: T)
  * nodes of sequence b exist.  Lengths read from device memory are clamped to the host-side bounds of the parameters.
+ * The threads of a launch are counted in 32 bits: problems that need more are SSV_EUNSUPPORTED.
  */
 #ifndef SSV_ROUND_H
 #define SSV_ROUND_H
@@ -46,6 +47,8 @@ typedef struct ssv_prefix_params {
  *   prefix_lens [n_prefix], seq_lens [B], n_query [B] or NULL, tree_parents [B,T] or NULL: device int32.
  *   Rows of out of nodes i >= n_query[b] are 0.  Rows beyond the lengths may hold anything; a row that some node of the
  *   sequence attends to must hold finite values.
+ *   Up to 2^19 sequences (and prefixes) times KV heads times groups of rows, a group being 16 of a sequence's T H / H_kv rows (or of those
+ *   of a prefix's sequences), of more than 16 rows 256 (bf16) or 32 (fp32); else SSV_EUNSUPPORTED, as are rows 32 MiB apart and more.
  *   workspace: >= ssv_prefix_workspace_bytes(p) bytes, 256-byte aligned; contents need not be preserved or initialised;
  *   calls sharing a workspace must not overlap in time.
  * Scores, softmax statistics and sums are fp32; with bf16 inputs the probabilities are rounded to bf16 for the matrix

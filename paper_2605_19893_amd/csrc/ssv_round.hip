@@ -28,6 +28,7 @@ bool repeats(int64_t extent, int64_t stride) { return extent > 1 && stride == 0;
 // ---- shared-prefix attention
 constexpr int kPrefixMaxSlices = kPrefixMaxSlots / 2;      // per part (prefix, own rows)
 constexpr int kPrefixWgs = 256;            // one round of workgroups: one per CU
+constexpr int64_t kPrefixMaxGroups = 1 << 19;      // (cache, KV head, row group) per part: with a slice each, both parts fit a launch
 
 struct PartPlan {
     int caches, per, rows, path, n_rg;
@@ -52,7 +53,7 @@ int plan_rows(PartPlan* pt, bool bf16, int H_kv) {
     pt->by_length = pt->caches > 1 && pt->caches <= kPrefixMaxDealt;
     pt->path = pt->rows <= 16 ? 1 : (bf16 ? 0 : 2);
     pt->n_rg = ceil_div(pt->rows, pt->path ? 16 * pt->path : 256);
-    return launchable(2 * ((int64_t)pt->caches * H_kv * pt->n_rg * kPrefixMaxSlices + 8), kPrefixThreads) ? SSV_OK : SSV_EUNSUPPORTED;
+    return (int64_t)pt->caches * H_kv * pt->n_rg <= kPrefixMaxGroups ? SSV_OK : SSV_EUNSUPPORTED;
 }
 
 // What a part would cost in a number of slices: workgroups, and microseconds of the longest and of an average one.  A rough model
@@ -127,6 +128,7 @@ void plan_slices(PrefixLayout* lo, const ssv_prefix_params* p) {
         const float idle = rest ? kPrefixWgs - rest : 0, done = (full + (rest ? 1 : 0)) * first.us;
         for (int j = 0; j < n_own; ++j) {
             const SliceCost& c = own[j];
+            if (!launchable((int64_t)first.wgs + c.wgs + 16, kPrefixThreads)) break;      // (more slices of these are more still; one each always fits)
             float us = done + spread_us(c, c.wgs, kPrefixWgs);       // behind the prefix's workgroups, or in the idle places of their last round
             if (idle > 0) us = std::min(us, std::max(done, full * first.us + spread_us(c, c.wgs, idle)));
             us += ((float)first.units * lo->part[0].rows + (float)c.units * lo->part[1].rows) * p->H_kv * state_us;

@@ -321,3 +321,30 @@ def test_largest_scores_pick_the_largest(shape, T):
     assert scale * np.abs(h["kp"][0, 0] @ h["q"][0, 0, 0]).max() > 2.0 ** 25
     rnd = 2.0 ** -8 if h["dt"] == "bf16" else 2.0 ** -24
     assert (np.abs(got - want) <= rnd * (mass + np.abs(want)) + 2.0 ** -22 * mass).all()
+
+
+def test_thousands_of_sequences():
+    """A batch whose sequences and KV heads are 2^16 and more (compared on the device, in 64 bits)."""
+    import torch
+    from paper_2605_19893_amd import binding as Bd
+    Bn, Hk, d, P, S = 8200, 8, 64, 70, 5
+    g = torch.Generator(device="cuda").manual_seed(46)
+    rnd = lambda *s: torch.randn(s, generator=g, device="cuda").bfloat16()
+    q, kp, vp, k, v = rnd(Bn, 1, Hk, d), rnd(1, Hk, P, d), rnd(1, Hk, P, d), rnd(Bn, Hk, S + 1, d), rnd(Bn, Hk, S + 1, d)
+    lens = (torch.arange(Bn, device="cuda") % (S + 1)).int()
+    p = Bd.make_prefix_params(B=Bn, T=1, H=Hk, H_kv=Hk, d_k=d, d_v=d, max_prefix_len=P, max_seq_len=S, kp_stride=kp.stride()[:3], vp_stride=vp.stride()[:3],
+                              k_stride=k.stride()[:3], v_stride=v.stride()[:3])
+    need = Bd.ssv_prefix_workspace_bytes(p)
+    assert need > 0
+    out, ws = torch.full_like(q, 7.0), torch.full((need,), 0x55, dtype=torch.uint8, device="cuda")
+    call([q, kp, vp, k, v, torch.tensor([P - 1], dtype=torch.int32, device="cuda"), lens, None, None, p, out, ws, need])
+    keys = torch.cat([kp[:, :, :P - 1].expand(Bn, -1, -1, -1), k], 2).double()
+    vals = torch.cat([vp[:, :, :P - 1].expand(Bn, -1, -1, -1), v], 2).double()
+    x = (keys * q[:, 0, :, None].double()).sum(3) * d ** -0.5
+    x = x.masked_fill((torch.arange(P + S, device="cuda") - (P - 1) > lens[:, None])[:, None], float("-inf"))
+    w = torch.softmax(x, 2)[..., None]
+    want, mass = (w * vals).sum(2), (w * vals.abs()).sum(2)
+    # (the tolerance of check())
+    size = (keys.abs() * q[:, 0, :, None].double().abs()).sum(3).amax(2)[..., None] * d ** -0.5
+    tol = 2 * ((d + 4) * 2.0 ** -24 * size + 2.0 ** -22 + (P + S) * 2.0 ** -24) * mass + 2.0 ** -8 * (mass + want.abs())
+    assert ((out[:, 0].double() - want).abs() <= tol).all()

@@ -241,3 +241,13 @@ def test_prefix_refuses_scales_above_2_to_the_100():
     test_prefix_refusals(dict(scale=2.0 ** 100 * (1 + 2.0 ** -23)), B.SSV_EUNSUPPORTED)
     test_prefix_refusals(dict(scale=2.5e38), B.SSV_EUNSUPPORTED)
     test_prefix_refusals(dict(scale=3.4e38), B.SSV_EUNSUPPORTED)
+
+
+@pytest.mark.parametrize("over", [dict(B=8192, H=8, H_kv=8), dict(B=1 << 16, H=8, H_kv=8), dict(B=8192, H=8, H_kv=8, n_prefix=8192), dict(B=8192, H=64, H_kv=8, T=16),
+                                  dict(B=1 << 16, H=8, H_kv=8, max_prefix_len=100000, max_seq_len=100000)])
+def test_prefix_accepts_many_sequences(over):
+    """Up to 2^19 sequences times KV heads: what counts is the launch that the call makes, not the one with the most slices."""
+    kw = dict(T=1, n_prefix=1, d_k=64, d_v=64, kp_stride=(0, 0, 64), vp_stride=(0, 0, 64), k_stride=(0, 0, 64), v_stride=(0, 0, 64))
+    kw.update(over)
+    assert B.ssv_prefix_workspace_bytes(prefix_params(**kw)) > 0
+    test_prefix_refusals({**kw, "B": kw["B"] * 64, "n_prefix": kw["n_prefix"] * 64}, B.SSV_EUNSUPPORTED)
