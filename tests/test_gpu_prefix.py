@@ -348,3 +348,44 @@ def test_thousands_of_sequences():
     size = (keys.abs() * q[:, 0, :, None].double().abs()).sum(3).amax(2)[..., None] * d ** -0.5
     tol = 2 * ((d + 4) * 2.0 ** -24 * size + 2.0 ** -22 + (P + S) * 2.0 ** -24) * mass + 2.0 ** -8 * (mass + want.abs())
     assert ((out[:, 0].double() - want).abs() <= tol).all()
+
+
+@pytest.mark.parametrize("shape", ["bf16_192", "bf16_128", "bf16_64"])
+def test_sharp_scores_of_many_rows(shape):
+    """As test_scale_and_sharp_scores, with rows enough in both parts that they share the key tiles."""
+    args, h = setup(43, shape, B=2, T=9, H=8, Hk=2, G=1, plens=[300], lens=[50, 20], scale=0.9, sharp=4.0)
+    call(args)
+    check(args, h)
+
+
+@pytest.mark.parametrize("shape", ["bf16_192", "bf16_128", "bf16_64"])
+def test_scores_that_rise_from_tile_to_tile(shape):
+    """Rows that share key tiles, their reference maximum too low in every tile but a slice's first: one head's scores rise by a factor of
+    2^5.5 from one tile of 64 keys to the next (the tiles before keep a share of 2 %), one's by 2^14, one's fall, one's stay; the draft keys
+    come highest.  The values tell even tiles from odd ones."""
+    import torch
+    B, T, H, Hk, P, lens, step = 2, 9, 8, 2, 1000, [700, 333], 8.0
+    args, h = setup(44, shape, B=B, T=T, H=H, Hk=Hk, G=1, plens=[P], lens=lens, garbage=False, scale=0.0625, sharp=0.15)
+    d, n_tiles = h["dk"], (P - 1) // 64
+    factor = np.array([7.625, 19.5, -7.625, 0.0])
+    h["q"][..., 0] = factor[np.arange(H) % 4]
+    slot = np.arange(h["k"].shape[2])
+    h["kp"][0, :, :, 0] = step * (np.arange(P) // 64 - n_tiles)
+    h["vp"][0] += 2.0 * (1 - 2 * (np.arange(P) // 64 % 2))[:, None]
+    for b in range(B):
+        h["k"][b, :, :, 0] = np.where(slot < lens[b], step * (slot // 64 - lens[b] // 64), 2 * step)
+        h["v"][b] += 2.0 * (1 - 2 * (slot // 64 % 2))[:, None]
+    for at, name in ((0, "q"), (1, "kp"), (2, "vp"), (3, "k"), (4, "v")):
+        args[at].copy_(torch.from_numpy(h[name]).bfloat16())
+        h[name] = args[at].double().cpu().numpy()
+    # a lane holds the keys 32 kb + 8 j + 4 hb + r (hb = 0, 1) of a tile; against the largest score before the tile they sum to more than 512
+    for b in range(B):
+        for head in (0, 1, 4, 5):
+            for keys, n in ((h["kp"][0, head // 4], P), (h["k"][b, head // 4], lens[b])):
+                x = h["scale"] / np.log(2.0) * (keys[:n] @ h["q"][b, :, head].T)
+                for t in range(1, n // 64):
+                    for hb in range(2):
+                        mine = [64 * t + 32 * kb + 8 * j + 4 * hb + r for kb in range(2) for j in range(4) for r in range(4)]
+                        assert (np.exp2(x[mine] - x[:64 * t].max(0)).sum(0) > 600).all()
+    call(args)
+    check(args, h)
