@@ -131,3 +131,110 @@ def test_rounds(fanout):
         for x, y in zip(want, [lp.out, lp.tokens, lp.path, *lp.state()]):
             assert torch.equal(x, y)
         torch.randn(1000, device="cuda").sum().item()
+
+
+@pytest.mark.parametrize("fanout", [None, (3, 2, 1)])
+def test_rounds_of_sparse_attention(fanout, oracle):
+    """The same loop around the library's own attention: ssv_nsa_verify on a compressed cache that every round extends by what it committed."""
+    import dataclasses
+
+    import torch
+    from oracle import compress as oc
+    from paper_2605_19893_amd import binding as Bd
+    from paper_2605_19893_amd.device_case import DeviceCase
+    from parity import check, compare
+    start = [1400, 1023, 31]
+    parents = None if fanout is None else si.tree_parents(fanout, "bfs")
+    T = 8 if parents is None else len(parents)
+    nq = [T, T - 2, T]
+    nsa, n, Hk, d = si.NsaParams(n_sel=8, w=256), 3, 2, 64
+    case = si.make_case("sparse_rounds", "bf16", n, T, 16, Hk, d, d, nsa, [x + T * ROUNDS for x in start], 147, rho=0.5, parents=parents, n_query=nq,
+                        cmp_over_drafts=False)
+    dev = DeviceCase(case)
+    ints = lambda x: torch.as_tensor(np.asarray(x, np.int32)).cuda()
+    g = torch.Generator().manual_seed(78)
+    w, u = torch.randn((16 * d, VOCAB), generator=g).cuda(), torch.rand((n, T), generator=g).cuda()
+    draft, root = ints(np.random.default_rng(2).integers(0, VOCAB, (n, T))), ints([0, 1, 1])
+    logits, tokens, path, count = torch.zeros((n, T, VOCAB), device="cuda"), ints(np.full((n, T), -9)), ints(np.full((n, T), -9)), ints([0] * n)
+    before, new_lens = ints([0] * n), ints(start)
+    dev.seq_lens.copy_(new_lens)
+    dev.k_cmp.zero_()
+    dev.v_cmp.zero_()
+    sp = Bd.make_sample_params(B=n, T=T, V=VOCAB, dtype=Bd.SSV_F32)
+    need = Bd.ssv_sample_workspace_bytes(sp)
+    ws = torch.full((need,), 0x55, dtype=torch.uint8, device="cuda")
+    strides = dict(k_stride=dev.k.stride()[:3], v_stride=dev.v.stride()[:3])
+    cp = Bd.make_commit_params(B=n, T=T, H_kv=Hk, d_k=d, d_v=d, dtype=Bd.SSV_BF16, kv_capacity=dev.k.shape[2],
+                               k_stride=(0, *strides["k_stride"]), v_stride=(0, *strides["v_stride"]))
+    zp = Bd.make_cmp_params(B=n, H_kv=Hk, d_k=d, d_v=d, l=nsa.l, d=nsa.d, dtype=Bd.SSV_BF16, max_new_rows=dev.k_cmp.shape[2], kv_capacity=dev.k.shape[2],
+                            cmp_capacity=dev.k_cmp.shape[2], kc_stride=dev.k_cmp.stride()[:3], vc_stride=dev.v_cmp.stride()[:3], **strides)
+
+    def compress(s):
+        Bd.ssv_nsa_compress(dev.k, dev.v, dev.k_cmp, dev.v_cmp, before, new_lens, dev.n_cmp, zp, s)
+        before.copy_(new_lens)
+        dev.seq_lens.copy_(new_lens)
+
+    def attend_and_sample():
+        s = torch.cuda.current_stream().cuda_stream
+        dev.run()
+        torch.matmul(dev.out.reshape(n, T, 16 * d).float(), w, out=logits)
+        Bd.ssv_sample(logits, None, None, None, None, u, dev.n_query, sp, tokens, None, ws, need, s)
+
+    def accept_and_commit():
+        s = torch.cuda.current_stream().cuda_stream
+        Bd.ssv_accept(draft, root, tokens, dev.seq_lens, dev.n_query, dev.parents, n, T, path, count, root, new_lens, s)
+        Bd.ssv_commit(dev.k, dev.v, path, count, dev.seq_lens, cp, s)
+        compress(s)
+
+    kept = [dev.k, dev.v, dev.k_cmp, dev.v_cmp, dev.n_cmp, dev.seq_lens, before, new_lens, root]
+    compress(torch.cuda.current_stream().cuda_stream)
+    begin, after, accepted = [x.clone() for x in kept], [], 0
+    bits = lambda x: x.view(torch.int16).cpu().numpy().view(np.uint16)
+    f = lambda x: x.double().cpu().numpy()
+    tree = list(range(-1, T - 1)) if parents is None else [int(p) for p in parents]
+    for r in range(ROUNDS):
+        lens, first = dev.seq_lens.cpu().numpy(), root.tolist()
+        assert dev.n_cmp.tolist() == [oc.n_cmp_rows(int(x), nsa.l, nsa.d) for x in lens]
+        attend_and_sample()
+        out, sel = dev.results()
+        now = dataclasses.replace(case, name=f"sparse_rounds_{r}", seq_lens=lens, n_cmp=dev.n_cmp.cpu().numpy(), k=bits(dev.k), v=bits(dev.v),
+                                  k_cmp=bits(dev.k_cmp), v_cmp=bits(dev.v_cmp))
+        check(now, compare(now, oracle, oracle.nsa_verify(now), out, sel))
+        said, x, given = tokens.tolist(), f(logits), u.double().tolist()
+        for b in range(n):
+            for i in range(T):
+                token, _, margin = ro.sample(x[b, i], 1.0, 0, 1.0, 0.0, given[b][i]) if i < nq[b] else (-1, 0, 1.0)
+                assert margin < 2.0 ** -40 or said[b][i] == token
+        k0, v0 = f(dev.k), f(dev.v)
+        accept_and_commit()
+        torch.cuda.synchronize()
+        for b in range(n):
+            line, token, length = ro.accept(draft[b].tolist(), first[b], said[b], int(lens[b]), nq[b], tree)
+            assert path[b].tolist() == line + [-1] * (T - len(line)) and root[b].item() == token and dev.seq_lens[b].item() == length
+            accepted += len(line)
+            rows = oc.n_cmp_rows(length, nsa.l, nsa.d)
+            for c in range(Hk):
+                for was, moved, pooled in ((k0, dev.k, dev.k_cmp), (v0, dev.v, dev.v_cmp)):
+                    want = ro.commit(was[b, c], line, len(line), int(lens[b]), T, was.shape[2])
+                    assert np.array_equal(f(moved[b, c]), want)
+                    means = oc.compress(want, 0, length, nsa.l, nsa.d, "bf16")[2]
+                    assert (np.abs(f(pooled[b, c, :rows]) - means) <= 2.0 ** -8 * np.abs(means) + 33 * 2.0 ** -24 * np.abs(want[:length]).max()).all()
+        after.append([dev.out.clone(), dev.sel_idx.clone(), tokens.clone(), path.clone()] + [x.clone() for x in kept])
+    assert accepted > 0
+    # the same rounds from one graph
+    for x, y in zip(kept, begin):
+        x.copy_(y)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        attend_and_sample()
+        accept_and_commit()
+    for x, y in zip(kept, begin):
+        x.copy_(y)
+    for want in after:
+        graph.replay()
+        torch.cuda.synchronize()
+        for x, y in zip(want, [dev.out, dev.sel_idx, tokens, path] + kept):
+            assert torch.equal(x, y)
+        torch.randn(1000, device="cuda").sum().item()
