@@ -13,10 +13,11 @@
 //   keys path (prefix_keys): 16 rows (fp32: up to 32); the wavefronts divide the keys instead, nothing is shared: bound by memory.
 //
 // Measured (kernel alone, MI355X): chains of 16 in 32 sequences of 64 heads behind 32768 shared and 2048 own rows, 192 + 128:
-// 578 us, 1.23 PFLOP/s, what a large matrix product of the library reaches on the same card; one token each in 32 sequences
-// behind 16411 + 1024: 36.5 us for 92 MB and 22 GFLOP (18 us of either): the own keys, bound by memory, run after the prefix, bound
-// by the matrix cores, and 7 us pass before the first tile and after the last; four sequences behind 2048 + 128: 9.2 us, all
-// of it latency; fp32 chains of five behind 4097 + 300: 17.5 us.
+// 582 to 592 us apart from each other, 1.20 to 1.22 PFLOP/s, where a large matrix product of the library reaches 1.25 on the same
+// card (up to 684 us in some dozen launches one behind the other); one token each in 32 sequences behind 16411 + 1024: 36.8 us
+// for 92 MB and 22 GFLOP (18 us of either): 160 workgroups have 13 prefix tiles each, 27 us on the matrix cores, 96 of the 128 that
+// stream own keys run beside them on the other CUs and the last 32 behind, and 7 us pass before the first tile and after the last; four
+// sequences behind 2048 + 128: 9.4 us, all of it latency; fp32 chains of five behind 4097 + 300: 17.2 us.
 #pragma once
 #include <type_traits>
 

@@ -10,10 +10,13 @@
 // maximum's key.  k_sample_pick, one workgroup per row, finds the token from these: without filters by the block in which the
 // running sum passes u, of which alone the logits are read again; with filters from a list of candidates in LDS, the logits above
 // a bound that no kept entry can lie below (from histograms of the chunks' maxima), and only the histogram bin in which the
-// threshold falls is ordered.  Rows whose filters keep more than the list holds take the general way, radix selections over the row.
+// threshold falls is ordered.  Rows with more candidates than the list holds take the general way, radix selections that read the row again for
+// every digit: rows whose filters keep more than that, rows with more in the threshold's bin than is sorted, and rows whose top-k
+// is above the number of chunks that hold a finite logit (every logit is a candidate there: 1000 of 6000, say).
 //
-// Measured (kernels alone, MI355X; blocks + pick): 512 rows of 100003 fp32 logits without filters 47.5 + 8.5 us, 4.3 TB/s where
-// 5.1 is a copy's: fifteen 64-bit instructions per logit take half as long as the bytes; 128 rows of 131071 bf16 logits with
+// Measured (kernels alone, MI355X; blocks + pick): 512 rows of 100003 fp32 logits without filters 51 + 8.8 us, 4.0 TB/s where
+// 5.1 is a copy's: fifteen 64-bit instructions per logit take more than half as long as the bytes, and the pick holds its eight logits per
+// thread in scratch memory (8.4 MB written); 128 rows of 131071 bf16 logits with
 // mixed settings 13 + 20 us, the second for the rows that keep about a thousand (3.5 us the bound, 2.2 the chunks, 3.5 their
 // logits, 7 the thresholds: some fifteen barriers, LDS round trips and code that runs once); 8 rows of 32000 4.5 + 8 us, all of it latency.
 #pragma once
@@ -236,7 +239,7 @@ __device__ __forceinline__ Found<V> find_prefix(const V* part, int n, int lane, 
 }
 
 // One wavefront per block of 2048 logits, four blocks per workgroup.  Seven wavefronts to a SIMD (72 registers) hide the reads behind the
-// exponentials: 512 rows of 100003 fp32 logits take 47.5 us; 53.5 with three (142 registers), 35.5 without the exponentials, 40 a copy's time.
+// exponentials: 512 rows of 100003 fp32 logits take 51 us; 53.3 with three, 35.5 without the exponentials, 40 a copy's time.
 template <bool BF16>
 __global__ void __launch_bounds__(kThreads, 7) k_sample_blocks(const SampleArgs a) {
     touch_args<SampleArgs>();
