@@ -516,7 +516,7 @@ __global__ void __launch_bounds__(kSampleThreads) k_sample_pick(const SampleArgs
     // A weight in fixed point: sums of these do not depend on the order of the atomics.  The unit is the power of two that brings the sum of
     // what is added up to 2^62 .. 2^63, so that V roundings to it are at most V 2^-63 of that sum, however peaked the row is.  (A unit
     // made for V weights of 1 leaves the tail of a peaked row a few bits: of 2^20 entries behind a peak, of which top-p 0.9999999 keeps
-    // 214736, it kept 11000 fewer.)  Without top-k the sum is the row's, known from its blocks.
+    // 214736, it kept 320161.)  Without top-k the sum is the row's, known from its blocks.
     auto mass_scale_of = [](double sum) { return __builtin_ldexp(1.0, 63 - __builtin_amdgcn_frexp_exp(sum)); };      // sum below 2^exp
     double mass_scale = rule.by_p && !rule.by_k ? mass_scale_of(total) : 0.0;
     auto mass = [&](uint32_t k) { return (uint64_t)(weight(key_value(k)) * mass_scale + 0.5); };
