@@ -88,7 +88,7 @@ typedef struct ssv_sample_params {
  *   workspace: >= ssv_sample_workspace_bytes(p) bytes, 256-byte aligned, as in ssv_prefix_verify.
  * Weights and their sums are computed in 64 bits: a token of a large vocabulary has a weight far below the rounding of a 32-bit
  * sum, and a rounding of the running sum moves every border behind it.  The sums that top_p is compared with are 64-bit integers,
- * off by V 2^-63 of the whole sum at most; with top_k of up to 4096 by 2^-40 of the sum over the first top_k at most.
+ * off by V 2^-63 of the whole sum at most, with top_k by 2^-40 of the sum over the first top_k at most.
  */
 int ssv_sample(const void* logits, const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p,
                const float* u, const int32_t* n_query, const ssv_sample_params* p, int32_t* tokens, float* probs,
